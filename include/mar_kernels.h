@@ -17,6 +17,7 @@
 #ifndef MAR_KERNELS_H
 #define MAR_KERNELS_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #include "mar_cache.h"
@@ -114,6 +115,109 @@ mar_status mar_k_select_most_similar(const double* scores, int32_t n_slots, int3
  * Not thread-safe with concurrent launches. */
 #define MAR_GEMM_VARIANTS 16
 mar_status mar_k_gemm_variant(int32_t variant);
+
+/* ---------------------------------------------------------------------------
+ * Positions, the paged key/value cache and its attention: next to the slots of
+ * one fixed length above, a cache whose sequences grow page by page (several
+ * images or frames after each other, prompts of any length), share key/value
+ * heads between query heads, and may be causal.
+ *
+ * Rows of a batch are ragged: sequence s owns rows q_start[s] ..
+ * q_start[s + 1] - 1 of every row matrix, its n new tokens, and holds
+ * kv_len[s] tokens with them: its row i is token kv_len[s] - n + i.  Row
+ * matrices have a row stride of their own (`ld`, elements), so that the column
+ * blocks of one product's output can be passed in place.
+ *
+ * What a kernel reads from the device it bounds itself: an entry of `table`
+ * outside [0, n_pages) names no page (its keys are not visible, what is stored
+ * there is dropped), tokens below 0 or at max_kv and above are not stored and
+ * not visible, rows of no sequence (behind the last one, at m and above) are
+ * left as they were.  q_start must ascend; otherwise which sequence a row
+ * belongs to is undefined, but nothing outside the buffers is touched. */
+
+/* Which elements of a head make pair i of its n_pairs pairs: */
+typedef enum {
+  MAR_ROTARY_HALVES = 0,    /* (i, i + n_pairs) */
+  MAR_ROTARY_NEIGHBOURS = 1 /* (2 i, 2 i + 1) */
+} mar_rotary_layout;
+
+/* Rotary positions: pair i of every head of a row turns by the angle
+ *   pos[row, axis[i]] * freq[i]   (radians, reduced in fp64),
+ * (a, b) -> (a cos - b sin, b cos + a sin); elements from 2 n_pairs on stay.
+ * The axes are the caller's (time, height, width, ...): pairs may be divided
+ * among them in any way.  An axis outside [0, n_axes) leaves its pairs as they
+ * are; negated frequencies turn back. */
+typedef struct {
+  const double* freq;  /* device [n_pairs] */
+  const int32_t* axis; /* device [n_pairs] */
+  int32_t n_pairs;     /* multiple of 8, 8 <= n_pairs <= d_head / 2 */
+  int32_t n_axes;      /* 1 .. 4 */
+  int32_t layout;      /* mar_rotary_layout */
+} mar_rotary;
+
+/* The pages of a cache and a batch of sequences that live in them.  Token t of
+ * sequence s is row t % page of page table[s, t / page].  Pages of one
+ * sequence need no order, and sequences may share pages that none of them
+ * stores to.  k, v: 16-byte aligned.  page: a power of two, 16 .. 4096.
+ * d_head: a multiple of 16, 16 .. 128.  max_kv bounds every kv_len
+ * (1 <= max_kv <= max_pages * page <= 2^30): work is divided for that many
+ * keys.  n_seqs <= 65536. */
+typedef struct {
+  void *k, *v;            /* device [n_pages, n_heads, page, d_head] in dtype */
+  const int32_t* table;   /* device [n_seqs, max_pages] */
+  const int32_t* q_start; /* device [n_seqs + 1] */
+  const int32_t* kv_len;  /* device [n_seqs], the new tokens included */
+  int32_t n_pages, n_heads, page, d_head, n_seqs, max_pages, max_kv;
+} mar_paged_batch;
+
+/* out[m, n_heads * d_head] = rotary positions of the rows of x (head h at
+ * columns h * d_head ...), pos [m, n_axes] int32.  fp32 arithmetic, one
+ * rounding.  ld_x, ld_out: multiples of 8, at least n_heads * d_head; x and
+ * out 16-byte aligned; out may be x itself (same pointer and stride), else
+ * they must not overlap.  m * n_heads < 2^30. */
+mar_status mar_k_rotary(int32_t dtype, const mar_rotary* rotary, const void* x, int64_t ld_x,
+                        const int32_t* pos, int32_t m, int32_t n_heads, int32_t d_head, void* out,
+                        int64_t ld_out, void* stream);
+
+/* New tokens into the cache: keys k (rotated) and values v, [m, batch->n_heads
+ * * d_head] each, go to their pages; with q given, its n_heads_q heads are
+ * rotated into q_out (which may be q itself).  rotary NULL (pos is then
+ * ignored): no rotation, keys are stored and queries copied as they are.
+ * Strides and alignment as in mar_k_rotary.  Two rows must not name the same
+ * place in the cache. */
+mar_status mar_k_paged_store(int32_t dtype, const mar_paged_batch* batch, const mar_rotary* rotary,
+                             const int32_t* pos, int32_t m, const void* k, int64_t ld_k, const void* v,
+                             int64_t ld_v, int32_t n_heads_q, const void* q, int64_t ld_q, void* q_out,
+                             int64_t ld_q_out, void* stream);
+
+/* Attention of every row of the batch over its sequence's tokens in the cache:
+ * q, out [m, n_heads_q * d_head], n_heads_q a multiple of batch->n_heads (query
+ * head h reads key/value head h / (n_heads_q / batch->n_heads)), scale
+ * 1/sqrt(d_head), softmax statistics in fp32.  The row at token p sees token j
+ * of its sequence if
+ *   j < kv_len,  (not causal, or j <= p),
+ *   (window == 0, or j > p - window, or j < sinks):
+ * with a window the last `window` tokens up to its own, and the first `sinks`
+ * ones; without `causal` every token after it too.  A row that sees no token
+ * becomes zeros; what unseen tokens hold (infinities, NaN) does not matter.
+ * out must not overlap q or the pages.
+ *
+ * workspace: device, 16-byte aligned, of mar_k_paged_attention_workspace_bytes
+ * (or NULL with 0 bytes): where few rows read long sequences, their keys are
+ * divided among workgroups that leave their parts there.  A smaller one will
+ * do, with fewer parts and in less haste.  Calls that may overlap (on two
+ * streams, in two graphs) need a workspace each.  Sums are taken in an order
+ * that depends on the host's arguments and the lengths alone: equal calls give
+ * equal bits. */
+mar_status mar_k_paged_attention(int32_t dtype, const mar_paged_batch* batch, int32_t m, int32_t n_heads_q,
+                                 const void* q, int64_t ld_q, int32_t causal, int32_t window, int32_t sinks,
+                                 void* workspace, size_t workspace_bytes, void* out, int64_t ld_out,
+                                 void* stream);
+
+/* Bytes of workspace that mar_k_paged_attention makes use of (0 if none, or if
+ * an argument is refused; mar_last_error() then says why). */
+size_t mar_k_paged_attention_workspace_bytes(int32_t dtype, const mar_paged_batch* batch, int32_t m,
+                                             int32_t n_heads_q, int32_t window, int32_t sinks);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ MAR_F32, MAR_BF16 = 0, 1
 MAR_FULL, MAR_TOKEN_CACHED, MAR_TOKEN_GIVEN, MAR_TOKEN_CACHED_MOST_SIMILAR = 0, 1, 2, 3
 MAR_CFG_STORE, MAR_CFG_REUSE = 0, 1
 MAR_SCORE_VALUES, MAR_SCORE_FEATURES = 0, 1
+MAR_ROTARY_HALVES, MAR_ROTARY_NEIGHBOURS = 0, 1
 PROF_KINDS = ("qkv", "proj", "fc1", "fc2", "attention", "layernorm", "scores", "select", "cfg")
 
 STATUS_NAMES = {0: "MAR_OK", -1: "MAR_E_ARG", -2: "MAR_E_SHAPE", -3: "MAR_E_STATE",
@@ -32,6 +33,7 @@ EXPORTED = (
     "mar_k_layernorm", "mar_k_linear", "mar_k_linear_residual", "mar_k_qkv",
     "mar_k_attention", "mar_k_scores", "mar_k_select", "mar_k_select_most_similar",
     "mar_k_gemm_variant",
+    "mar_k_rotary", "mar_k_paged_store", "mar_k_paged_attention", "mar_k_paged_attention_workspace_bytes",
     "mar_head_workspace_bytes", "mar_head_init", "mar_head_sample", "mar_head_destroy",
     "mar_head_sample_noalloc",
 )
@@ -76,7 +78,19 @@ class MarHeadWeightsC(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in HEAD_WEIGHT_FIELDS]
 
 
+class MarRotaryC(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("n_pairs", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+class MarPagedBatchC(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "table", "q_start", "kv_len")] +
+                [(n, ctypes.c_int32) for n in ("n_pages", "n_heads", "page", "d_head", "n_seqs", "max_pages",
+                                               "max_kv")])
+
+
 _vp, _i32, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+_i64 = ctypes.c_int64
 _SIGNATURES = {
     "mar_workspace_bytes": (_sz, [ctypes.POINTER(MarDimsC)]),
     "mar_cache_init": (_i32, [ctypes.POINTER(MarDimsC), ctypes.POINTER(MarBlockWeightsC), _vp, _sz, _vp,
@@ -100,6 +114,12 @@ _SIGNATURES = {
     "mar_k_select": (_i32, [_vp, _i32, _i32, _i32, _vp, _vp]),
     "mar_k_select_most_similar": (_i32, [_vp, _i32, _i32, _i32, _vp, _vp]),
     "mar_k_gemm_variant": (_i32, [_i32]),
+    "mar_k_rotary": (_i32, [_i32, ctypes.POINTER(MarRotaryC), _vp, _i64, _vp, _i32, _i32, _i32, _vp, _i64, _vp]),
+    "mar_k_paged_store": (_i32, [_i32, ctypes.POINTER(MarPagedBatchC), ctypes.POINTER(MarRotaryC), _vp, _i32, _vp,
+                                 _i64, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "mar_k_paged_attention": (_i32, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _i32, _vp, _i64, _i32, _i32, _i32,
+                                     _vp, _sz, _vp, _i64, _vp]),
+    "mar_k_paged_attention_workspace_bytes": (_sz, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _i32, _i32, _i32]),
     "mar_head_workspace_bytes": (_sz, [ctypes.POINTER(MarHeadDimsC)]),
     "mar_head_init": (_i32, [ctypes.POINTER(MarHeadDimsC), ctypes.POINTER(MarHeadWeightsC), _vp, _sz, _vp,
                              ctypes.POINTER(_vp)]),
@@ -316,6 +336,182 @@ def k_select(scores, n: int, idx, stream=None, most_similar: bool = False) -> No
 def k_gemm_variant(variant: int) -> None:
     """Force a tile configuration of the matrix products (-1: by shape)."""
     _check(load().mar_k_gemm_variant(variant))
+
+
+# --------------------------------------------------------------------------
+# rotary positions, the paged cache and its attention
+# --------------------------------------------------------------------------
+
+def _refuse(message: str) -> None:
+    raise MarError(MAR_E_ARG, message)
+
+
+def _dense(name: str, t, dtype, shape, device) -> None:
+    """t is a dense tensor of this type and shape (None: any size) on `device`."""
+    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+        _refuse(f"{name}: need a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        _refuse(f"{name}: shape {tuple(t.shape)} is not {shape}")
+
+
+def _rows(name: str, t, dtype, m: int, d_head: int, device) -> int:
+    """t is a matrix of m rows of whole heads on `device`, its columns dense: the
+    number of heads."""
+    if t.dtype != dtype or t.device != device:
+        _refuse(f"{name}: need a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+    if t.dim() != 2 or t.shape[0] != m or t.shape[1] % d_head or (t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"{name}: need {m} rows of whole heads of {d_head} dense columns, got {tuple(t.shape)}")
+    return t.shape[1] // d_head
+
+
+def _stride(t) -> int:
+    """Row stride; a single row has none of its own, so it counts as dense."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _here(device) -> None:
+    torch = _torch()
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        _refuse(f"the tensors are on {device}: need the current GPU")
+
+
+def _storage_code(dtype) -> int:
+    torch = _torch()
+    if dtype not in (torch.float32, torch.bfloat16):
+        _refuse(f"unsupported storage type {dtype}")
+    return MAR_F32 if dtype == torch.float32 else MAR_BF16
+
+
+LAYOUTS = {"halves": MAR_ROTARY_HALVES, "neighbours": MAR_ROTARY_NEIGHBOURS}
+
+
+def rotary_sections(sections: Sequence[int], base: float = 10000.0, shared: bool = False, device="cuda"):
+    """(freq, axis) of `Rotary` for sections[a] pairs of axis a, one after the
+    other: pair j of a section of n turns base^(-j / n) per position, as where
+    every axis has the whole range of frequencies; with `shared` pair i of all P
+    pairs turns base^(-i / P), as where the axes divide one range."""
+    torch = _torch()
+    P = sum(sections)
+    axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    power = [i / P for i in range(P)] if shared else [j / n for n in sections for j in range(n)]
+    return (torch.tensor([base ** -p for p in power], dtype=torch.float64, device=device),
+            torch.tensor(axis, dtype=torch.int32, device=device))
+
+
+class Rotary:
+    """Rotary positions: freq [pairs] fp64 (radians per position; negated ones
+    turn back), axis [pairs] int32, layout "halves" (pair i is elements i and
+    i + pairs) or "neighbours" (2 i and 2 i + 1)."""
+
+    def __init__(self, freq, axis, n_axes: int, layout: str = "halves"):
+        torch = _torch()
+        if layout not in LAYOUTS:
+            _refuse(f"unknown layout {layout!r}")
+        _dense("freq", freq, torch.float64, (None,), freq.device)
+        _dense("axis", axis, torch.int32, (freq.shape[0],), freq.device)
+        self.freq, self.axis, self.n_axes = freq, axis, n_axes
+        self.c = MarRotaryC(freq.data_ptr(), axis.data_ptr(), freq.shape[0], n_axes, LAYOUTS[layout])
+
+
+class MarPages:
+    """The pages of a cache: k and v [n_pages, heads, page, d_head]."""
+
+    def __init__(self, k, v):
+        _storage_code(k.dtype)
+        _dense("k", k, k.dtype, (None, None, None, None), k.device)
+        _dense("v", v, k.dtype, tuple(k.shape), k.device)
+        self.k, self.v = k, v
+
+
+class PagedBatch:
+    """Sequences that live in `pages`: table [seqs, max_pages], q_start [seqs +
+    1] and kv_len [seqs], all int32.  The tensors are held and read at every
+    call, so their contents may change from step to step; max_kv bounds every
+    kv_len (None: what the table's row holds)."""
+
+    def __init__(self, pages: MarPages, table, q_start, kv_len, max_kv: Optional[int] = None):
+        torch = _torch()
+        dev = pages.k.device
+        _dense("table", table, torch.int32, (None, None), dev)
+        _dense("q_start", q_start, torch.int32, (table.shape[0] + 1,), dev)
+        _dense("kv_len", kv_len, torch.int32, (table.shape[0],), dev)
+        n_pages, heads, page, d_head = pages.k.shape
+        self.pages, self.table, self.q_start, self.kv_len = pages, table, q_start, kv_len
+        self.dtype, self.device, self.d_head = pages.k.dtype, dev, d_head
+        self.code = _storage_code(pages.k.dtype)
+        self.c = MarPagedBatchC(pages.k.data_ptr(), pages.v.data_ptr(), table.data_ptr(), q_start.data_ptr(),
+                                kv_len.data_ptr(), n_pages, heads, page, d_head, table.shape[0], table.shape[1],
+                                table.shape[1] * page if max_kv is None else max_kv)
+
+
+def k_rotary(rotary: Rotary, x, pos, out, d_head: int, stream=None) -> None:
+    """out = rotary positions pos [m, n_axes] int32 on the rows of x
+    [m, heads * d_head]; out may be x."""
+    torch = _torch()
+    m, dev = x.shape[0], rotary.freq.device
+    heads = _rows("x", x, x.dtype, m, d_head, dev)
+    if _rows("out", out, x.dtype, m, d_head, dev) != heads:
+        _refuse("out and x differ in width")
+    _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
+    _here(dev)
+    _check(load().mar_k_rotary(_storage_code(x.dtype), ctypes.byref(rotary.c), x.data_ptr(), _stride(x),
+                               pos.data_ptr(), m, heads, d_head, out.data_ptr(), _stride(out), _stream(stream)))
+
+
+def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[Rotary] = None, pos=None,
+                  stream=None) -> None:
+    """Keys k (rotated) and values v [m, heads * d_head] of the batch's new
+    tokens into its pages; q, if given, rotated into q_out (which may be q)."""
+    torch = _torch()
+    m, dev, dh = k.shape[0], batch.device, batch.d_head
+    for name, t in (("k", k), ("v", v)):
+        if _rows(name, t, batch.dtype, m, dh, dev) != batch.c.n_heads:
+            _refuse(f"{name}: need {batch.c.n_heads} heads of {dh}")
+    heads = ldq = ldo = 0
+    if q is not None:
+        heads = _rows("q", q, batch.dtype, m, dh, dev)
+        if q_out is None or _rows("q_out", q_out, batch.dtype, m, dh, dev) != heads:
+            _refuse("q needs a q_out of its width")
+        ldq, ldo = _stride(q), _stride(q_out)
+    if rotary is not None:
+        if pos is None or rotary.freq.device != dev:
+            _refuse("rotary needs pos, and its tables on the batch's GPU")
+        _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
+    _here(dev)
+    _check(load().mar_k_paged_store(batch.code, ctypes.byref(batch.c),
+                                    None if rotary is None else ctypes.byref(rotary.c), _ptr(pos), m, k.data_ptr(),
+                                    _stride(k), v.data_ptr(), _stride(v), heads, _ptr(q), ldq,
+                                    _ptr(q_out) if q is not None else None, ldo, _stream(stream)))
+
+
+def paged_attention_workspace_bytes(batch: PagedBatch, m: int, n_heads_q: int, window: int = 0,
+                                    sinks: int = 0) -> int:
+    """Bytes of workspace that k_paged_attention makes use of for up to m rows."""
+    lib = load()
+    n = lib.mar_k_paged_attention_workspace_bytes(batch.code, ctypes.byref(batch.c), m, n_heads_q, window, sinks)
+    if n == 0 and lib.mar_last_error():
+        raise MarError(MAR_E_ARG, lib.mar_last_error().decode())
+    return n
+
+
+def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: int = 0, sinks: int = 0,
+                      workspace=None, stream=None) -> None:
+    """Attention of the rows q [m, heads * d_head] over their sequences' tokens
+    in the pages; workspace: a tensor of any type (see
+    paged_attention_workspace_bytes) or None."""
+    m, dev, dh = q.shape[0], batch.device, batch.d_head
+    heads = _rows("q", q, batch.dtype, m, dh, dev)
+    if _rows("out", out, batch.dtype, m, dh, dev) != heads:
+        _refuse("out and q differ in width")
+    ws_bytes = 0
+    if workspace is not None:
+        if workspace.device != dev or not workspace.is_contiguous():
+            _refuse("workspace: need a contiguous tensor on the batch's GPU")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _here(dev)
+    _check(load().mar_k_paged_attention(batch.code, ctypes.byref(batch.c), m, heads, q.data_ptr(), _stride(q),
+                                        1 if causal else 0, window, sinks, _ptr(workspace) if ws_bytes else None,
+                                        ws_bytes, out.data_ptr(), _stride(out), _stream(stream)))
 
 
 # --------------------------------------------------------------------------

@@ -1,0 +1,215 @@
+// Rotary positions, and new tokens into the pages of the cache.
+//
+// Memory-bound: every element is read once and written once.  A workgroup
+// takes a few consecutive rows: first the cosines and sines of their pairs
+// (once per row, shared by all its heads) and the rows' places in the cache go
+// to LDS, then its threads walk the heads in units of 16 elements.  A unit
+// holds 8 whole pairs in either layout, so a thread reads all that it turns
+// before it writes, and the result may overwrite the input.
+//
+// Angles: pos * freq in fp64, in quarter turns, reduced to [-1/2, 1/2] there
+// and only then rounded to fp32 (positions reach 2^30, where an fp32 angle
+// would be off by whole turns); sine and cosine of the rest in fp32.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace marcache {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxRows = 16;  // rows of a workgroup
+constexpr int kMaxPairs = 64;
+
+struct RowArgs {
+  RotaryArgs rot;
+  PagedBatch b;  // STORE only
+  const void *q, *k, *v;
+  void* q_out;
+  long ld_q, ld_k, ld_v, ld_q_out;
+  int m, heads_q, d_head, rows;  // rows of a workgroup
+  int first;                     // row of workgroup 0
+  Divisor by_units, by_heads;    // d_head / 16 units of a head; heads of a row
+};
+
+__device__ __forceinline__ float2 turn(int pos, double freq) {
+  const double t = static_cast<double>(pos) * (freq * 0.63661977236758134308);  // quarter turns
+  const double n = __builtin_rint(t);
+  const int quadrant = static_cast<int>(n - 4.0 * __builtin_floor(n * 0.25));
+  float s, c;
+  sincospif(0.5f * static_cast<float>(t - n), &s, &c);
+  if (quadrant & 1) {
+    const float w = c;
+    c = -s;
+    s = w;
+  }
+  return quadrant & 2 ? make_float2(-c, -s) : make_float2(c, s);
+}
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float* x) {
+  unpack16(*reinterpret_cast<const u32x4_t*>(p), x, static_cast<const T*>(nullptr));
+  if constexpr (sizeof(T) == 4)
+    unpack16(*reinterpret_cast<const u32x4_t*>(p + 4), x + 4, static_cast<const T*>(nullptr));
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float* x) {
+  u32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pack2bf(x[2 * i], x[2 * i + 1]);
+  *reinterpret_cast<u32x4_t*>(p) = v;
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    *reinterpret_cast<f32x4_t*>(p + 4 * i) = f32x4_t{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+}
+
+template <typename T, bool STORE>
+__global__ __launch_bounds__(kThreads) void rows_kernel(const RowArgs a) {
+  __shared__ float2 cs[kMaxRows * kMaxPairs];
+  __shared__ long place[kMaxRows];  // element of the row's first key in the pages, or -1
+  __shared__ int owned[kMaxRows];   // the row belongs to a sequence
+  const int row0 = a.first + blockIdx.x * a.rows;
+  const int rows = min(a.rows, a.m - row0);
+  const int P = a.rot.freq ? a.rot.n_pairs : 0;
+  for (int i = threadIdx.x; i < rows * P; i += kThreads) {
+    const int r = i / P, p = i - r * P;
+    const int ax = a.rot.axis[p];
+    cs[r * kMaxPairs + p] = ax < 0 || ax >= a.rot.n_axes
+                                ? make_float2(1.f, 0.f)
+                                : turn(a.rot.pos[static_cast<long>(row0 + r) * a.rot.n_axes + ax], a.rot.freq[p]);
+  }
+  if constexpr (STORE) {
+    if (threadIdx.x < static_cast<unsigned>(rows)) {
+      const int row = row0 + threadIdx.x;
+      int lo = 0, n = a.b.n_seqs;  // the last sequence that starts at or before the row
+      while (n > 1) {
+        const int half = n >> 1;
+        const bool right = a.b.q_start[lo + half] <= row;
+        lo = right ? lo + half : lo;
+        n = right ? n - half : half;
+      }
+      const SeqSpan s = seq_span(a.b, lo, a.m);
+      const bool mine = row >= s.row0 && row < s.row0 + s.n;
+      const int t = s.first + row - s.row0;
+      long at = -1;
+      if (mine && t >= 0 && t < s.len) {
+        const int page = a.b.table[static_cast<long>(lo) * a.b.max_pages + (t >> a.b.page_shift)];
+        if (page >= 0 && page < a.b.n_pages)
+          at = ((static_cast<long>(page) * a.b.n_heads << a.b.page_shift) + (t & ((1 << a.b.page_shift) - 1))) *
+               a.d_head;
+      }
+      place[threadIdx.x] = at;
+      owned[threadIdx.x] = mine;
+    }
+  }
+  __syncthreads();
+  const int units = a.d_head / 16;
+  const int heads = a.heads_q + (STORE ? 2 * a.b.n_heads : 0);
+  for (int i = threadIdx.x; i < rows * heads * units; i += kThreads) {
+    const int rh = div_by(i, a.by_units.magic, a.by_units.shift), u = i - rh * units;
+    const int r = div_by(rh, a.by_heads.magic, a.by_heads.shift), h = rh - r * heads;
+    const long row = row0 + r;
+    const T* src;
+    T* dst;
+    bool turned = u < P / 8;
+    if (h < a.heads_q) {
+      if (STORE && !owned[r]) continue;
+      src = static_cast<const T*>(a.q) + row * a.ld_q + h * a.d_head;
+      dst = static_cast<T*>(a.q_out) + row * a.ld_q_out + h * a.d_head;
+    } else {
+      if (place[r] < 0) continue;
+      int hk = h - a.heads_q;
+      const bool value = hk >= a.b.n_heads;
+      if (value) hk -= a.b.n_heads;
+      turned = turned && !value;
+      src = (value ? static_cast<const T*>(a.v) + row * a.ld_v : static_cast<const T*>(a.k) + row * a.ld_k) +
+            hk * a.d_head;
+      dst = static_cast<T*>(value ? a.b.v : a.b.k) + place[r] + (static_cast<long>(hk) * a.d_head << a.b.page_shift);
+    }
+    const bool halves = turned && !a.rot.neighbours;
+    const int e0 = halves ? 8 * u : 16 * u, e1 = halves ? P + 8 * u : 16 * u + 8;
+    float x[16], y[16];
+    load8(src + e0, x);
+    load8(src + e1, x + 8);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) y[j] = x[j];
+    if (turned) {
+      const float2* c = cs + r * kMaxPairs + 8 * u;
+      if (halves) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          y[j] = fmaf(x[j], c[j].x, -x[8 + j] * c[j].y);
+          y[8 + j] = fmaf(x[8 + j], c[j].x, x[j] * c[j].y);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          y[2 * j] = fmaf(x[2 * j], c[j].x, -x[2 * j + 1] * c[j].y);
+          y[2 * j + 1] = fmaf(x[2 * j + 1], c[j].x, x[2 * j] * c[j].y);
+        }
+      }
+    }
+    store8(dst + e0, y);
+    store8(dst + e1, y + 8);
+  }
+}
+
+template <bool STORE>
+hipError_t launch_rows(int dtype, RowArgs& a, hipStream_t st) {
+  const int heads = a.heads_q + (STORE ? 2 * a.b.n_heads : 0);
+  if (a.m == 0 || heads == 0 || (STORE && a.b.n_seqs == 0)) return hipSuccess;
+  a.rows = 1;
+  a.by_units = make_divisor(a.d_head / 16);
+  a.by_heads = make_divisor(heads);
+  const long grid = (static_cast<long>(a.m) + a.rows - 1) / a.rows;
+  for (long first = 0; first < grid; first += kMaxGrid) {
+    a.first = static_cast<int>(first * a.rows);
+    const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, grid - first)));
+    if (dtype == DT_BF16)
+      hipLaunchKernelGGL((rows_kernel<bf16_t, STORE>), part, dim3(kThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL((rows_kernel<float, STORE>), part, dim3(kThreads), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_rotary(int dtype, const RotaryArgs& rot, const void* x, long ld_x, int m, int heads, int d_head,
+                         void* out, long ld_out, hipStream_t st) {
+  RowArgs a{};
+  a.rot = rot;
+  a.q = x;
+  a.ld_q = ld_x;
+  a.q_out = out;
+  a.ld_q_out = ld_out;
+  a.m = m;
+  a.heads_q = heads;
+  a.d_head = d_head;
+  return launch_rows<false>(dtype, a, st);
+}
+
+hipError_t launch_paged_store(int dtype, const PagedBatch& b, const RotaryArgs& rot, int m, const void* k, long ld_k,
+                              const void* v, long ld_v, int heads_q, const void* q, long ld_q, void* q_out,
+                              long ld_q_out, hipStream_t st) {
+  RowArgs a{};
+  a.rot = rot;
+  a.b = b;
+  a.q = q;
+  a.ld_q = ld_q;
+  a.q_out = q_out;
+  a.ld_q_out = ld_q_out;
+  a.k = k;
+  a.ld_k = ld_k;
+  a.v = v;
+  a.ld_v = ld_v;
+  a.m = m;
+  a.heads_q = heads_q;
+  a.d_head = b.d_head;
+  return launch_rows<true>(dtype, a, st);
+}
+
+}  // namespace marcache
