@@ -161,7 +161,7 @@ typedef struct {
  * stores to.  k, v: 16-byte aligned.  page: a power of two, 16 .. 4096.
  * d_head: a multiple of 16, 16 .. 128.  max_kv bounds every kv_len
  * (1 <= max_kv <= max_pages * page <= 2^30): work is divided for that many
- * keys.  n_seqs <= 65536. */
+ * keys.  n_heads <= 4096, n_seqs <= 65536. */
 typedef struct {
   void *k, *v;            /* device [n_pages, n_heads, page, d_head] in dtype */
   const int32_t* table;   /* device [n_seqs, max_pages] */

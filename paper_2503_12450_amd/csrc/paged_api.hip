@@ -62,7 +62,7 @@ mar_status take_batch(const mar_paged_batch* b, PagedBatch* out) {
   if (!b) return fail(MAR_E_ARG, "batch is NULL");
   mar_status s = check_head(b->d_head);
   if (s != MAR_OK) return s;
-  if (b->n_heads < 1 || b->n_heads > 65536) return fail(MAR_E_SHAPE, "batch: n_heads %d outside [1, 65536]", b->n_heads);
+  if (b->n_heads < 1 || b->n_heads > 4096) return fail(MAR_E_SHAPE, "batch: n_heads %d outside [1, 4096]", b->n_heads);
   if (b->n_seqs < 0 || b->n_seqs > 65536) return fail(MAR_E_SHAPE, "batch: n_seqs %d outside [0, 65536]", b->n_seqs);
   if (b->page < 16 || b->page > 4096 || (b->page & (b->page - 1)))
     return fail(MAR_E_SHAPE, "batch: page %d must be a power of two, 16..4096", b->page);

@@ -1,7 +1,22 @@
 // Attention of a ragged batch of rows over a paged cache.
 //
-// One workgroup per (row, query head): 256 keys at a time, one per thread,
-// with an online softmax; then the threads share the values' columns.
+// The rows of a sequence that read one key/value head (its n new tokens times
+// the `group` query heads that share the head) are packed, row R = token R /
+// group, head R % group, and cut into tiles; a workgroup takes a tile of one
+// sequence and head and walks the keys that any of its rows sees: first the
+// sinks, then the window, in blocks, with an online softmax.  The softmax
+// state of a row stays in the lanes that own it; what a row does not see
+// inside a block is masked there, and blocks that no row sees are not read.
+//
+//   attn_many  128 rows, 32 to each of four waves, which share the key blocks
+//              (prompts, frames, chunks)
+//   attn_few   32 rows, held by each of four waves, which divide the keys
+//              (single tokens and few rows: bound by reading the cache once)
+//   attn_f32   16 rows on the fp32 MFMAs, the keys divided over the waves
+//
+// Where there are too few tiles to fill the chip, the key blocks of a tile are
+// further divided among workgroups, which leave their rows' maximum, sum and
+// output in the workspace for attn_join.
 #include <algorithm>
 
 #include "paged.h"
@@ -10,100 +25,955 @@ namespace marcache {
 
 namespace {
 
-template <typename T>
-__global__ __launch_bounds__(256) void paged_attn_kernel(const PagedBatch b, const T* __restrict__ q, long ld_q,
-                                                         T* __restrict__ out, long ld_out, int m, int heads_q,
-                                                         bool causal, int window, int sinks, float scale_log2, unsigned first) {
-  constexpr int KB = 256;
-  __shared__ float qs[128], ps[KB], part[256], red[8];
-  __shared__ long off[KB];
-  const unsigned block = first + blockIdx.x;
-  const int row = block / heads_q, h = block - row * heads_q;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int dh = b.d_head, hk = h / (heads_q / b.n_heads);
-  int s = 0, n = b.n_seqs;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kInf = __builtin_huge_valf();
+constexpr int kWaves = 4;
+constexpr int kGroup = 16;  // keys that always lie in one page
+
+struct AttnArgs {
+  PagedBatch b;
+  const void* q;
+  void* out;
+  long ld_q, ld_out;
+  int m, heads_q, group;
+  Divisor by_group;
+  int causal, window, sinks;
+  float scale_log2;
+  int tile_rows;          // packed rows of a tile
+  int tiles;              // bound of the tiles of all sequences
+  int parts, part_blocks; // workgroups that share a tile, blocks of keys of each
+  float* ws_ml;           // [m * heads_q][parts][2]
+  float* ws_o;            // [m * heads_q][parts][d_head]
+  unsigned first;         // work item of workgroup 0
+};
+
+// A tile: rows [r0, r0 + n) of the packed rows of sequence s.
+struct Tile {
+  SeqSpan sp;
+  int s, r0, n;
+};
+
+// The last sequence with key(s) <= at, where key ascends with s and key(0) = 0:
+// a wave probes 64 places at once.
+template <typename F>
+__device__ __forceinline__ int wave_search(int n_seqs, int at, F&& key) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = n_seqs;
   while (n > 1) {
-    const int half = n >> 1;
-    const bool right = b.q_start[s + half] <= row;
-    s = right ? s + half : s;
-    n = right ? n - half : half;
+    const int step = (n + 63) >> 6;
+    const int i = lane * step;
+    const bool in = i < n && key(lo + i) <= at;
+    const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(in)) - 1, 0);
+    lo += k * step;
+    n = min(step, n - k * step);
   }
-  const SeqSpan sp = seq_span(b, s, m);
-  if (row < sp.row0 || row >= sp.row0 + sp.n) return;
-  const int p = sp.first + row - sp.row0;
-  const int hi = causal ? min(sp.len, p + 1) : sp.len;
-  const int lo = window > 0 ? max(0, p - min(window, kMaxTokens) + 1) : 0;
-  if (tid < dh) qs[tid] = Elem<T>::to_f(q[row * ld_q + h * dh + tid]) * scale_log2;
-  const T* kp = static_cast<const T*>(b.k);
-  const T* vp = static_cast<const T*>(b.v);
-  const int page_mask = (1 << b.page_shift) - 1;
-  float m_run = -__builtin_huge_valf(), l_run = 0.f, acc = 0.f;
-  const int lanes_d = 256 / dh;  // threads that share a column
-  const int d = tid % dh, sub = tid / dh;
-  for (int j0 = 0; j0 < hi; j0 += KB) {
-    if (j0 + KB <= lo && j0 >= sinks) continue;
-    __syncthreads();
-    const int j = j0 + tid;
-    long at = -1;
-    if (j < hi && (j >= lo || j < sinks)) {
-      const int page = b.table[static_cast<long>(s) * b.max_pages + (j >> b.page_shift)];
-      if (page >= 0 && page < b.n_pages)
-        at = (((static_cast<long>(page) * b.n_heads + hk) << b.page_shift) + (j & page_mask)) * dh;
+  return lo;
+}
+
+// Tiles are numbered so that sequence s starts at floor(its first packed row /
+// tile_rows) + s: numbers ascend, no two sequences share one, and the few that
+// name no rows end at once.  Needs no pass over the lengths.
+__device__ __forceinline__ int first_tile(const AttnArgs& a, int s) {
+  return min(max(a.b.q_start[s], 0), a.m) * a.group / a.tile_rows + s;
+}
+__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int t) {
+  Tile r;
+  r.s = __builtin_amdgcn_readfirstlane(wave_search(a.b.n_seqs, t, [&](int s) { return first_tile(a, s); }));
+  r.sp = seq_span(a.b, r.s, a.m);
+  r.r0 = (t - first_tile(a, r.s)) * a.tile_rows;
+  r.n = r.r0 < 0 ? 0 : min(a.tile_rows, r.sp.n * a.group - r.r0);
+  return r;
+}
+
+// Keys that the row at token p sees: [lo, hi) and those below sinks (and hi).
+__device__ __forceinline__ int row_hi(const AttnArgs& a, const SeqSpan& sp, int p) {
+  return a.causal ? min(sp.len, p + 1) : sp.len;
+}
+__device__ __forceinline__ int row_lo(const AttnArgs& a, int p) {
+  return a.window ? max(0, p - a.window + 1) : 0;
+}
+
+// The blocks of KB keys that a tile reads: blocks 0 .. sink_blocks - 1, then
+// from block0 on, `count` together.
+struct Blocks {
+  int sink_blocks, block0, count;
+  __device__ __forceinline__ int at(int i) const { return i < sink_blocks ? i : block0 + i - sink_blocks; }
+};
+__device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const Tile& t, int kb) {
+  const int p0 = t.sp.first + div_by(t.r0, a.by_group.magic, a.by_group.shift);
+  const int p1 = t.sp.first + div_by(t.r0 + t.n - 1, a.by_group.magic, a.by_group.shift);
+  const int hi = max(row_hi(a, t.sp, p1), 0), lo = row_lo(a, p0);
+  Blocks r;
+  r.block0 = lo / kb;
+  r.sink_blocks = min((min(a.sinks, hi) + kb - 1) / kb, r.block0);
+  r.count = r.sink_blocks + max((hi + kb - 1) / kb - r.block0, 0);
+  return r;
+}
+
+// The pages of 64 consecutive groups of 16 keys, one to a lane, from group 64 *
+// batch on: one load per 1024 keys.  Groups past the table's row, and entries
+// that name no page, are marked invalid and read page 0, whose keys are then
+// masked.
+struct PageWindow {
+  int batch = -1, page = 0;
+  uint64_t valid = 0;
+  __device__ __forceinline__ void seek(const PagedBatch& b, int s, int group) {
+    if (group >> 6 == batch) return;
+    batch = group >> 6;
+    const int slot = ((batch << 6) + static_cast<int>(threadIdx.x & 63)) >> (b.page_shift - 4);
+    const bool in = slot < b.max_pages;
+    page = b.table[static_cast<long>(s) * b.max_pages + (in ? slot : 0)];
+    const bool ok = in && page >= 0 && page < b.n_pages;
+    valid = __builtin_amdgcn_ballot_w64(ok);
+    if (!ok) page = 0;
+  }
+  __device__ __forceinline__ int page_of(int group) const { return __builtin_amdgcn_readlane(page, group & 63); }
+  // validity of the n groups from `group` on, a bit per key
+  template <int N> __device__ __forceinline__ uint64_t keys(int group) const {
+    const uint64_t bits = valid >> (group & 63);
+    uint64_t r = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r |= (bits >> i & 1) ? uint64_t{0xFFFF} << (16 * i) : 0;
+    return r;
+  }
+};
+
+// First element of key `key` (a multiple of 16) of head hk on `page`.
+__device__ __forceinline__ long key_offset(const PagedBatch& b, int page, int hk, int key, int dh) {
+  return (((static_cast<long>(page) * b.n_heads + hk) << b.page_shift) + (key & ((1 << b.page_shift) - 1))) * dh;
+}
+
+// What a lane's row of a tile is.
+struct Row {
+  long q_at, out_at;  // element offsets in q and out
+  long part;          // index in the workspace
+  int hi, lo;
+  bool ok;
+};
+__device__ __forceinline__ Row make_row(const AttnArgs& a, const Tile& t, int hk, int i) {
+  Row r;
+  r.ok = i < t.n;
+  const int R = t.r0 + min(i, t.n - 1);
+  const int tok = div_by(R, a.by_group.magic, a.by_group.shift);
+  const int h = hk * a.group + R - tok * a.group;
+  const long row = t.sp.row0 + tok;
+  r.q_at = row * a.ld_q + static_cast<long>(h) * a.b.d_head;
+  r.out_at = row * a.ld_out + static_cast<long>(h) * a.b.d_head;
+  r.part = row * a.heads_q + h;
+  const int p = t.sp.first + tok;
+  r.hi = row_hi(a, t.sp, p);
+  r.lo = row_lo(a, p);
+  return r;
+}
+
+__device__ __forceinline__ int wave_min(int v) {
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
+
+// ---------------------------------------------------------------------------
+// bf16: 32 rows by 32 keys at a time on the 32x32x16 MFMAs, transposed so that
+// a row stays in one column (lane % 32) of both products:
+//   S^T (32 keys x 32 rows) = K Q^T,   O^T (32 d x 32 rows) += V^T P^T.
+// Lane (c, h) = (lane % 32, lane / 32) owns row c: S^T leaves it keys
+// 8 j + 4 h + i (register 4 j + i), which are the k-slots it feeds to the
+// second product; V^T follows that order through transposed LDS reads.
+// ---------------------------------------------------------------------------
+
+template <int DH>
+struct Geo {
+  static constexpr int DS = DH / 16;                                // k-steps of S^T
+  static constexpr int DT = (DH + 31) / 32;                         // 32-row tiles of O^T
+  static constexpr int CH = DH / 8;                                 // 16-byte chunks of a row
+  static constexpr int CHP = CH <= 4 ? 4 : (CH <= 8 ? 8 : 16);      // as laid out in LDS
+  static constexpr int ROW = 8 * CHP;                               // elements of a row in LDS
+  // A row's chunk c lies at c ^ swizzle(row), so that the rows that one LDS
+  // access reads fall on different banks: the keys' 16 rows x 1 chunk, the
+  // values' 4 rows x 4 chunks (of 16 chunks, a row of banks).
+  static __device__ __forceinline__ int k_swizzle(int row) {
+    return CHP == 16 ? row & 15 : (CHP == 8 ? (row >> 1) & 7 : (row >> 2) & 3);
+  }
+  static __device__ __forceinline__ int v_swizzle(int row) {
+    return CHP == 16 ? (row & 3) << 2 : (CHP == 8 ? (row >> 1 & 1) << 2 : 0);
+  }
+};
+
+template <int DH>
+struct RowState {
+  f32x16_t o[Geo<DH>::DT];
+  float m = -kInf;  // reference of the exponents, log2 units
+  float l = 0.f;    // this lane's share of the row's sum
+  __device__ __forceinline__ RowState() {
+#pragma unroll
+    for (int t = 0; t < Geo<DH>::DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  }
+};
+
+__device__ __forceinline__ u32x2_t read_tr(const bf16_t* p) {
+  typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+  return __builtin_bit_cast(
+      u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p)));
+}
+
+__device__ __forceinline__ bool not_finite(uint32_t two) {
+  return (two & 0x7F80u) == 0x7F80u || (two & 0x7F800000u) == 0x7F800000u;
+}
+__device__ __forceinline__ uint32_t finite_part(uint32_t two) {
+  if ((two & 0x7F80u) == 0x7F80u) two &= 0xFFFF0000u;
+  if ((two & 0x7F800000u) == 0x7F800000u) two &= 0xFFFFu;
+  return two;
+}
+
+// The values' fragments of NSB x 32 keys: element [sb][s2][t] holds keys 32 sb
+// + 16 s2 + {4 h + i, 8 + 4 h + i} of column 32 t + c.
+template <int DH, int NSB>
+__device__ __forceinline__ void load_values(const bf16_t* vs, int lane, u32x4_t (&vf)[NSB][2][Geo<DH>::DT]) {
+  using G = Geo<DH>;
+  const int row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  // row's swizzle does not change with the multiples of 8 added to it
+  const int sw = G::v_swizzle(row);
+#pragma unroll
+  for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int t = 0; t < G::DT; ++t) {
+        const bf16_t* p = vs + (32 * sb + 16 * s2 + row) * G::ROW + 8 * (((32 * t + col) >> 3) ^ sw) + (col & 7);
+        const u32x2_t lo = read_tr(p), hi = read_tr(p + 8 * G::ROW);
+        vf[sb][s2][t] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+      }
+}
+
+// One block of 32 NSB keys from key0 on, given its scores S^T: mask (unless
+// the whole wave sees the whole block), softmax step, second product.
+// `alive`: a bit per key whose page exists.
+template <int DH, int NSB, bool MASKED>
+__device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NSB], u32x4_t (&vf)[NSB][2][Geo<DH>::DT],
+                                             const bf16_t* vs, int key0, const Row& row, int sinks, uint64_t alive,
+                                             float scale_log2) {
+  using G = Geo<DH>;
+  const int lane = threadIdx.x & 63, hg = lane >> 5;
+  if constexpr (MASKED) {
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int at = 32 * sb + 8 * (r >> 2) + 4 * hg + (r & 3), key = key0 + at;
+        const bool seen = key < row.hi && (key >= row.lo || key < sinks) && (alive >> at & 1);
+        sc[sb][r] = seen ? sc[sb][r] : -kInf;
+      }
+  }
+  float tmax = -kInf;
+#pragma unroll
+  for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sc[sb][r]);
+  tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+  // p = 2^(s scale - m) for any reference m gives the same softmax, so a row's
+  // reference moves only when its maximum passes it by 2^8: p stays below 256.
+  // The decision is the row's own, the others of the wave multiply by 1.
+  const float m_blk = tmax * scale_log2;
+  const bool grow = m_blk > st.m + 8.f;
+  if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+    const float alpha = grow ? __builtin_amdgcn_exp2f(st.m - m_blk) : 1.f;
+    st.m = grow ? m_blk : st.m;
+    st.l *= alpha;
+#pragma unroll
+    for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[t][r] *= alpha;
+  }
+  const float ref = st.m == -kInf ? 0.f : st.m;  // no key seen yet: every p is 2^-inf
+  float psum = 0.f;
+#pragma unroll
+  for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[sb][r], scale_log2, -ref));
+      sc[sb][r] = p;
+      psum += p;
     }
-    float sc = -__builtin_huge_valf();
-    if (at >= 0) {
-      sc = 0.f;
-      for (int e = 0; e < dh; ++e) sc = fmaf(qs[e], Elem<T>::to_f(kp[at + e]), sc);
+  st.l += psum;
+  uint64_t odd = 0;  // keys whose value row is not finite throughout
+  if constexpr (MASKED) {
+    // 0 times an unseen infinity or NaN would spoil the row: such values leave
+    // the product, and are added to the rows that do see them
+    bool any = false;
+    if (lane < 32 * NSB)
+      for (int c = 0; c < G::CH; ++c) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(vs + lane * G::ROW + 8 * (c ^ G::v_swizzle(lane)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) any |= not_finite(x[i]);
+      }
+    odd = __builtin_amdgcn_ballot_w64(any);
+    if (odd) {
+#pragma unroll
+      for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+          for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vf[sb][s2][t][i] = finite_part(vf[sb][s2][t][i]);
     }
-    off[tid] = at;
-    float mx = sc;
-    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-    if (lane == 0) red[wave] = mx;
+  }
+#pragma unroll
+  for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      u32x4_t pf;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pf[i] = pack2bf(sc[sb][8 * s2 + 2 * i], sc[sb][8 * s2 + 2 * i + 1]);
+#pragma unroll
+      for (int t = 0; t < G::DT; ++t)
+        st.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[sb][s2][t]),
+                                                          __builtin_bit_cast(bf16x8_t, pf), st.o[t], 0, 0, 0);
+    }
+  if constexpr (MASKED) {
+    for (odd &= alive; odd; odd &= odd - 1) {
+      const int at = __builtin_ctzll(odd), key = key0 + at;
+      if (!(key < row.hi && (key >= row.lo || key < sinks))) continue;
+#pragma unroll
+      for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * t + 8 * j + 4 * hg;
+          const u32x2_t x = *reinterpret_cast<const u32x2_t*>(vs + at * G::ROW + 8 * ((d >> 3) ^ G::v_swizzle(at)) +
+                                                              4 * hg);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16;
+            if ((w & 0x7F800000u) == 0x7F800000u) st.o[t][4 * j + i] += __uint_as_float(w);
+          }
+        }
+    }
+  }
+}
+
+template <int DH>
+__device__ __forceinline__ void load_q(const AttnArgs& a, const Row& row, int hg, u32x4_t (&qf)[Geo<DH>::DS]) {
+  const bf16_t* q = static_cast<const bf16_t*>(a.q) + row.q_at;
+#pragma unroll
+  for (int st = 0; st < Geo<DH>::DS; ++st)
+    qf[st] = row.ok ? *reinterpret_cast<const u32x4_t*>(q + 16 * st + 8 * hg) : u32x4_t{0u, 0u, 0u, 0u};
+}
+
+// The lane's share of its row, finished or as a part: o[t][4 j + i] = O[32 t +
+// 8 j + 4 h + i].
+template <int DH>
+__device__ __forceinline__ void store_row(const AttnArgs& a, const Row& row, const RowState<DH>& st, float l, int hg,
+                                          int part) {
+  if (!row.ok) return;
+  if (a.parts > 1) {
+    const long at = row.part * a.parts + part;
+    if (hg == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(st.m, l);
+    float* o = a.ws_o + at * DH;
+#pragma unroll
+    for (int t = 0; t < Geo<DH>::DT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * t + 8 * j + 4 * hg;
+        if (d < DH)
+          *reinterpret_cast<f32x4_t*>(o + d) =
+              f32x4_t{st.o[t][4 * j], st.o[t][4 * j + 1], st.o[t][4 * j + 2], st.o[t][4 * j + 3]};
+      }
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
+  bf16_t* o = static_cast<bf16_t*>(a.out) + row.out_at;
+#pragma unroll
+  for (int t = 0; t < Geo<DH>::DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * t + 8 * j + 4 * hg;
+      if (d < DH)
+        *reinterpret_cast<u32x2_t*>(o + d) = u32x2_t{pack2bf(st.o[t][4 * j] * inv, st.o[t][4 * j + 1] * inv),
+                                                     pack2bf(st.o[t][4 * j + 2] * inv, st.o[t][4 * j + 3] * inv)};
+    }
+}
+
+// Work item -> (tile, head, part).  Heads run fastest: workgroups are dealt to
+// the eight XCDs in turn, so the tiles of one head meet in one L2.  Tiles run
+// backwards: with a causal mask the last ones are the longest.
+__device__ __forceinline__ void work_item(const AttnArgs& a, int& tile, int& hk, int& part) {
+  const unsigned w = a.first + blockIdx.x;
+  hk = w % a.b.n_heads;
+  const unsigned r = w / a.b.n_heads;
+  part = r % a.parts;
+  tile = a.tiles - 1 - r / a.parts;
+}
+__device__ __forceinline__ void part_range(const AttnArgs& a, int part, int count, int& from, int& to) {
+  from = part * a.part_blocks;
+  to = part == a.parts - 1 ? count : min(count, from + a.part_blocks);
+}
+
+// Sixteen bytes per lane into LDS at lds_addr + 16 * lane, from a wave-uniform
+// address and a lane's byte offset.  Issued from asm so that the compiler adds
+// no waits of its own; lds_arrived() waits.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(const void* base, int voff, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds_addr), "v"(voff), "s"(base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// This wave's copies are in LDS and its LDS reads are done; then all waves'.
+__device__ __forceinline__ void lds_arrived() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+// LDS operations of one wave execute in order; this keeps the compiler to it.
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+template <int DH>
+__global__ __launch_bounds__(64 * kWaves) void attn_many(const AttnArgs a) {
+  using G = Geo<DH>;
+  constexpr int KB = 64;                       // keys of a block
+  constexpr int RPI = 64 / G::CHP;             // rows that a wave copies at once
+  constexpr int COPIES = KB / (RPI * kWaves);  // times that it does
+  __shared__ __align__(16) bf16_t ks[2][KB * G::ROW];
+  __shared__ __align__(16) bf16_t vs[2][KB * G::ROW];
+  int tile_no, hk, part;
+  work_item(a, tile_no, hk, part);
+  const Tile tile = find_tile(a, tile_no);
+  if (tile.n <= 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hg = lane >> 5;
+  const Blocks blocks = tile_blocks(a, tile, KB);
+  int from, to;
+  part_range(a, part, blocks.count, from, to);
+  if (from >= to && from > 0) return;  // attn_join knows which parts there are
+  const Row row = make_row(a, tile, hk, wave * 32 + c);
+  u32x4_t qf[G::DS];
+  load_q<DH>(a, row, hg, qf);
+  // what the wave's rows see, for whole blocks
+  const int hi_min = wave_min(row.ok ? row.hi : 0x7FFFFFFF), hi_max = wave_max(row.ok ? row.hi : 0);
+  const int lo_min = wave_min(row.ok ? row.lo : 0x7FFFFFFF), lo_max = wave_max(row.ok ? row.lo : 0);
+
+  // The wave copies rows RPI (wave + 4 i) + lane / CHP of a block: they lie in
+  // one group of 16 keys, at an offset that depends on the lane alone.
+  const int in_group = (RPI * wave) % kGroup + lane / G::CHP;
+  const int copy_row = RPI * wave + lane / G::CHP;  // up to the multiples of 16 that i adds
+  const int chunk = lane % G::CHP;
+  const int koff = 2 * (in_group * DH + 8 * min(chunk ^ G::k_swizzle(copy_row), G::CH - 1));
+  const int voff = 2 * (in_group * DH + 8 * min(chunk ^ G::v_swizzle(copy_row), G::CH - 1));
+  const unsigned ks0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) bf16_t*)&ks[0][RPI * wave * G::ROW]));
+  const unsigned vs0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) bf16_t*)&vs[0][RPI * wave * G::ROW]));
+  PageWindow pages;
+  uint64_t alive_next = 0;
+  auto copy_block = [&](int i, int buf) {
+    const int group0 = blocks.at(i) * (KB / kGroup);
+    pages.seek(a.b, tile.s, group0);
+    alive_next = pages.keys<KB / kGroup>(group0);
+#pragma unroll
+    for (int k = 0; k < COPIES; ++k) {
+      const int group = group0 + RPI * (wave + kWaves * k) / kGroup;
+      const long at = key_offset(a.b, pages.page_of(group), hk, group * kGroup, DH);
+      const unsigned lds = 2u * (buf * KB * G::ROW + RPI * kWaves * k * G::ROW);
+      copy16(static_cast<const bf16_t*>(a.b.k) + at, koff, ks0 + lds);
+      copy16(static_cast<const bf16_t*>(a.b.v) + at, voff, vs0 + lds);
+    }
+  };
+
+  RowState<DH> st;
+  if (from < to) copy_block(from, 0);
+  for (int i = from; i < to; ++i) {
+    const int buf = (i - from) & 1;
+    lds_arrived();  // this block is here, and every wave has left the one before
+    const uint64_t alive = alive_next;
+    if (i + 1 < to) copy_block(i + 1, buf ^ 1);
+    const int key0 = blocks.at(i) * KB;
+    if (key0 >= hi_max || (key0 + KB <= lo_min && key0 >= a.sinks)) continue;  // not for this wave
+    const bf16_t* kb = ks[buf];
+    u32x4_t kf[2][G::DS];
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+      for (int s = 0; s < G::DS; ++s)
+        kf[sb][s] = *reinterpret_cast<const u32x4_t*>(kb + (32 * sb + c) * G::ROW +
+                                                      8 * ((2 * s + hg) ^ G::k_swizzle(c)));
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16_t sc[2];
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[sb][r] = 0.f;
+#pragma unroll
+      for (int s = 0; s < G::DS; ++s)
+        sc[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[sb][s]),
+                                                         __builtin_bit_cast(bf16x8_t, qf[s]), sc[sb], 0, 0, 0);
+    }
+    u32x4_t vf[2][2][G::DT];
+    load_values<DH, 2>(vs[buf], lane, vf);
+    __builtin_amdgcn_sched_barrier(0);
+    const bool whole = key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && alive == ~uint64_t{0};
+    if (whole)
+      softmax_step<DH, 2, false>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2);
+    else
+      softmax_step<DH, 2, true>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2);
+  }
+  const float l = st.l + __shfl_xor(st.l, 32, 64);
+  store_row<DH>(a, row, st, l, hg, part);
+}
+
+// 32 rows; wave w takes blocks w, w + 4, ... of 32 keys.  The keys go from
+// memory to the registers that feed the first product, the values through a
+// piece of LDS of the wave's own; both are loaded a block ahead.
+template <int DH>
+__global__ __launch_bounds__(64 * kWaves) void attn_few(const AttnArgs a) {
+  using G = Geo<DH>;
+  constexpr int KB = 32;
+  constexpr int RPI = 64 / G::CHP;     // value rows that a wave loads at once
+  constexpr int LOADS = KB / RPI;
+  constexpr int OROW = DH + 4;         // row stride of the outputs that waves exchange
+  constexpr int VBYTES = kWaves * KB * G::ROW * 2, OBYTES = (kWaves / 2) * 32 * (OROW + 2) * 4;
+  __shared__ __align__(16) unsigned char lds[VBYTES > OBYTES ? VBYTES : OBYTES];
+  int tile_no, hk, part;
+  work_item(a, tile_no, hk, part);
+  const Tile tile = find_tile(a, tile_no);
+  if (tile.n <= 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hg = lane >> 5;
+  const Blocks blocks = tile_blocks(a, tile, KB);
+  int from, to;
+  part_range(a, part, blocks.count, from, to);
+  if (from >= to && from > 0) return;
+  const Row row = make_row(a, tile, hk, c);
+  u32x4_t qf[G::DS];
+  load_q<DH>(a, row, hg, qf);
+  const int hi_min = wave_min(row.ok ? row.hi : 0x7FFFFFFF), lo_max = wave_max(row.ok ? row.lo : 0);
+  bf16_t* vs = reinterpret_cast<bf16_t*>(lds) + wave * KB * G::ROW;
+
+  PageWindow pages;
+  u32x4_t kf[G::DS], vr[LOADS];
+  uint64_t alive_next = 0;
+  const int vrow = lane / G::CHP, vchunk = lane % G::CHP;
+  auto load_block = [&](int i) {
+    const int group0 = blocks.at(i) * (KB / kGroup);
+    pages.seek(a.b, tile.s, group0);
+    alive_next = pages.keys<KB / kGroup>(group0);
+    const long at0 = key_offset(a.b, pages.page_of(group0), hk, group0 * kGroup, DH);
+    const long at1 = key_offset(a.b, pages.page_of(group0 + 1), hk, (group0 + 1) * kGroup, DH);
+    const bf16_t* kp = static_cast<const bf16_t*>(a.b.k) + (c < 16 ? at0 : at1) + (c & 15) * DH + 8 * hg;
+#pragma unroll
+    for (int s = 0; s < G::DS; ++s) kf[s] = *reinterpret_cast<const u32x4_t*>(kp + 16 * s);
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+      const int r = RPI * k;  // the rows of a load lie in one group
+      const bf16_t* vp = static_cast<const bf16_t*>(a.b.v) + (r < 16 ? at0 : at1) + (r % 16 + vrow) * DH;
+      vr[k] = *reinterpret_cast<const u32x4_t*>(vp + 8 * min(vchunk, G::CH - 1));
+    }
+  };
+  RowState<DH> st;
+  if (from + wave < to) load_block(from + wave);
+  for (int i = from + wave; i < to; i += kWaves) {
+    const uint64_t alive = alive_next;
+    const int key0 = blocks.at(i) * KB;
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k)
+      *reinterpret_cast<u32x4_t*>(vs + (RPI * k + vrow) * G::ROW + 8 * (vchunk ^ G::v_swizzle(RPI * k + vrow))) = vr[k];
+    f32x16_t sc[1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[0][r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < G::DS; ++s)
+      sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s]),
+                                                      __builtin_bit_cast(bf16x8_t, qf[s]), sc[0], 0, 0, 0);
+    if (i + kWaves < to) load_block(i + kWaves);
+    wave_order();
+    u32x4_t vf[1][2][G::DT];
+    load_values<DH, 1>(vs, lane, vf);
+    const bool whole =
+        key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && (alive & 0xFFFFFFFFu) == 0xFFFFFFFFu;
+    if (whole)
+      softmax_step<DH, 1, false>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2);
+    else
+      softmax_step<DH, 1, true>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2);
+    wave_order();
+  }
+  // Join the waves' rows in pairs: the upper half of them leaves maximum, sum
+  // and output in LDS, the lower half takes them in.
+  float l = st.l + __shfl_xor(st.l, 32, 64);
+  float* ol = reinterpret_cast<float*>(lds);
+  float* ml = ol + (kWaves / 2) * 32 * OROW;
+#pragma unroll
+  for (int half = kWaves / 2; half > 0; half >>= 1) {
     __syncthreads();
-    const float m_new = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), m_run);
-    const float ref = m_new == -__builtin_huge_valf() ? 0.f : m_new;
+    if (wave >= half && wave < 2 * half) {
+      float* o = ol + ((wave - half) * 32 + c) * OROW;
+#pragma unroll
+      for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * t + 8 * j + 4 * hg;
+          if (d < DH)
+            *reinterpret_cast<f32x4_t*>(o + d) =
+                f32x4_t{st.o[t][4 * j], st.o[t][4 * j + 1], st.o[t][4 * j + 2], st.o[t][4 * j + 3]};
+        }
+      if (hg == 0) {
+        ml[2 * ((wave - half) * 32 + c)] = st.m;
+        ml[2 * ((wave - half) * 32 + c) + 1] = l;
+      }
+    }
+    __syncthreads();
+    if (wave < half) {
+      const float* o = ol + (wave * 32 + c) * OROW;
+      const float m2 = ml[2 * (wave * 32 + c)], l2 = ml[2 * (wave * 32 + c) + 1];
+      const float m_new = fmaxf(st.m, m2), ref = m_new == -kInf ? 0.f : m_new;
+      const float f1 = __builtin_amdgcn_exp2f(st.m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+      st.m = m_new;
+      l = fmaf(l, f1, l2 * f2);
+#pragma unroll
+      for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * t + 8 * j + 4 * hg;
+          if (d < DH) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(o + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.o[t][4 * j + e] = fmaf(st.o[t][4 * j + e], f1, x[e] * f2);
+          }
+        }
+    }
+  }
+  if (wave == 0) store_row<DH>(a, row, st, l, hg, part);
+}
+
+// ---------------------------------------------------------------------------
+// fp32: 16 rows; wave w takes blocks w, w + 4, ... of 16 keys, with the fp32
+// 16x16x4 MFMAs: S^T (16 keys x 16 rows) = K Q^T, lane (c, g) = (lane % 16,
+// lane / 16) feeding key (row) c at d = g DH/4 + step; O^T (16 d x 16 rows) +=
+// V^T P^T, S^T leaving lane (c, g) with row c's keys 4 g + r.
+// ---------------------------------------------------------------------------
+template <int DH>
+__global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
+  constexpr int QB = 16, KB = 16;
+  constexpr int DL = DH / 4;    // floats of a row per lane
+  constexpr int DT = DH / 16;   // 16-row tiles of O^T
+  constexpr int OROW = DH + 1;
+  __shared__ float part_o[kWaves][QB * OROW];
+  __shared__ float part_m[kWaves][QB], part_l[kWaves][QB];
+  int tile_no, hk, part;
+  work_item(a, tile_no, hk, part);
+  const Tile tile = find_tile(a, tile_no);
+  if (tile.n <= 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const Blocks blocks = tile_blocks(a, tile, KB);
+  int from, to;
+  part_range(a, part, blocks.count, from, to);
+  if (from >= to && from > 0) return;
+  const Row row = make_row(a, tile, hk, c);
+  const int hi_min = wave_min(row.ok ? row.hi : 0x7FFFFFFF), lo_max = wave_max(row.ok ? row.lo : 0);
+  f32x4_t q[DL / 4];
+  {
+    const float* qr = static_cast<const float*>(a.q) + row.q_at + g * DL;
+#pragma unroll
+    for (int i = 0; i < DL / 4; ++i) q[i] = *reinterpret_cast<const f32x4_t*>(qr + 4 * i);
+  }
+  f32x4_t acc[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m_run = -kInf, l_run = 0.f;
+  PageWindow pages;
+  f32x4_t k[DL / 4];
+  float v[4][DT];  // V[key 4 g + r][16 t + c]
+  bool alive_next = false;
+  auto load_block = [&](int i) {
+    const int group = blocks.at(i);
+    pages.seek(a.b, tile.s, group);
+    alive_next = pages.keys<1>(group) != 0;
+    const long at = key_offset(a.b, pages.page_of(group), hk, group * kGroup, DH);
+    const float* kr = static_cast<const float*>(a.b.k) + at + c * DH + g * DL;
+#pragma unroll
+    for (int i2 = 0; i2 < DL / 4; ++i2) k[i2] = *reinterpret_cast<const f32x4_t*>(kr + 4 * i2);
+    const float* vr = static_cast<const float*>(a.b.v) + at + 4 * g * DH + c;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < DT; ++t) v[r][t] = vr[r * DH + 16 * t];
+  };
+  if (from + wave < to) load_block(from + wave);
+  for (int i = from + wave; i < to; i += kWaves) {
+    const int key0 = blocks.at(i) * KB;
+    const bool alive = alive_next;
+    f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < DL / 4; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e][j], q[e][j], sc, 0, 0, 0);
+    const bool whole = key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && alive;
+    uint32_t odd[4] = {0, 0, 0, 0};  // [r] bit g: key 4 g + r holds a value that is not finite
+    float x[4][DT];
+    if (!whole) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        bool any = false;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          x[r][t] = v[r][t];
+          const bool out = !(fabsf(v[r][t]) < kInf);
+          any |= out;
+          if (out) v[r][t] = 0.f;
+        }
+        const uint64_t who = __builtin_amdgcn_ballot_w64(any);
+#pragma unroll
+        for (int g2 = 0; g2 < 4; ++g2) odd[r] |= (who >> (16 * g2) & 0xFFFF) ? 1u << g2 : 0u;
+      }
+    }
+    float tmax = -kInf;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int key = key0 + 4 * g + r;
+      const bool seen = whole || (alive && key < row.hi && (key >= row.lo || key < a.sinks));
+      sc[r] = seen ? sc[r] * a.scale_log2 : -kInf;
+      tmax = fmaxf(tmax, sc[r]);
+    }
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+    const float m_new = fmaxf(m_run, tmax);
+    const float ref = m_new == -kInf ? 0.f : m_new;
     const float alpha = exp2f(m_run - ref);
-    const float e = at >= 0 ? exp2f(sc - ref) : 0.f;
-    ps[tid] = e;
-    const float sum = wave_sum(e);
-    if (lane == 0) red[4 + wave] = sum;
-    __syncthreads();
     m_run = m_new;
-    l_run = l_run * alpha + ((red[4] + red[5]) + (red[6] + red[7]));
-    acc *= alpha;
-    if (sub < lanes_d)
-      for (int t = sub; t < KB; t += lanes_d)
-        if (off[t] >= 0) acc = fmaf(ps[t], Elem<T>::to_f(vp[off[t] + d]), acc);
+    float p[4], psum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      p[r] = exp2f(sc[r] - ref);
+      psum += p[r];
+    }
+    l_run = fmaf(l_run, alpha, psum);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[t][r] *= alpha;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < DT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][t], p[r], acc[t], 0, 0, 0);
+    if (!whole && alive) {
+      // values that are not finite, for the rows that see their keys
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        for (uint32_t set = odd[r]; set; set &= set - 1) {
+          const int g2 = __builtin_ctz(set), key = key0 + 4 * g2 + r;
+          const bool seen = key < row.hi && (key >= row.lo || key < a.sinks);
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float y = __shfl(x[r][t], 16 * g2 + 4 * g + e, 64);
+              if (seen && !(fabsf(y) < kInf)) acc[t][e] += y;
+            }
+        }
+    }
+    if (i + kWaves < to) load_block(i + kWaves);
   }
-  part[tid] = acc;
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) part_o[wave][c * OROW + 16 * t + 4 * g + r] = acc[t][r];
+  if (g == 0) {
+    part_m[wave][c] = m_run;
+    part_l[wave][c] = l_run;
+  }
   __syncthreads();
-  if (tid < dh) {
-    float o = 0.f;
-    for (int t = 0; t < lanes_d; ++t) o += part[t * dh + tid];
-    out[row * ld_out + h * dh + tid] = Elem<T>::from_f(l_run == 0.f ? 0.f : o / l_run);
+  const int i = threadIdx.x >> 4;
+  if (i >= tile.n) return;
+  float m = part_m[0][i];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w][i]);
+  const float ref = m == -kInf ? 0.f : m;
+  float f[kWaves], l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    f[w] = exp2f(part_m[w][i] - ref);
+    l = fmaf(part_l[w][i], f[w], l);
   }
+  const Row mine = make_row(a, tile, hk, i);
+  const bool last = a.parts == 1;
+  const float inv = last ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
+  const long at = mine.part * a.parts + part;
+  float* out = last ? static_cast<float*>(a.out) + mine.out_at : a.ws_o + at * DH;
+  if (!last && (threadIdx.x & 15) == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(m, l);
+#pragma unroll
+  for (int t = 0; t < DT; ++t) {
+    const int d = 16 * t + (threadIdx.x & 15);
+    float o = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) o = fmaf(part_o[w][i * OROW + d], f[w], o);
+    out[d] = o * inv;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The parts of a row joined: a wave per row, in order of the parts.
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb) {
+  const long item = static_cast<long>(a.first) + static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (item >= static_cast<long>(a.m) * a.heads_q) return;
+  const int row = static_cast<int>(item / a.heads_q), h = static_cast<int>(item - static_cast<long>(row) * a.heads_q);
+  const int lane = threadIdx.x & 63;
+  Tile t;
+  t.s = wave_search(a.b.n_seqs, row, [&](int s) { return a.b.q_start[s]; });
+  t.sp = seq_span(a.b, t.s, a.m);
+  if (row < t.sp.row0 || row >= t.sp.row0 + t.sp.n) return;
+  const int R = (row - t.sp.row0) * a.group + h % a.group;
+  t.r0 = R / a.tile_rows * a.tile_rows;
+  t.n = min(a.tile_rows, t.sp.n * a.group - t.r0);
+  const int count = tile_blocks(a, t, kb).count;
+  const int parts = max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
+  const float* ml = a.ws_ml + 2 * item * a.parts;
+  float m = -kInf;
+  for (int p = lane; p < parts; p += 64) m = fmaxf(m, ml[2 * p]);
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float ref = m == -kInf ? 0.f : m;
+  const int dh = a.b.d_head;
+  const float* o = a.ws_o + item * a.parts * dh;
+  const int d = min(2 * lane, dh - 2);
+  float l = 0.f, x = 0.f, y = 0.f;
+  for (int p = 0; p < parts; ++p) {
+    const float f = exp2f(ml[2 * p] - ref);
+    l = fmaf(ml[2 * p + 1], f, l);
+    const float2 w = *reinterpret_cast<const float2*>(o + static_cast<long>(p) * dh + d);
+    x = fmaf(w.x, f, x);
+    y = fmaf(w.y, f, y);
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  if (2 * lane < dh) {
+    T* out = static_cast<T*>(a.out) + row * a.ld_out + static_cast<long>(h) * dh + d;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint32_t*>(out) = pack2bf(x * inv, y * inv);
+    else
+      *reinterpret_cast<float2*>(out) = make_float2(x * inv, y * inv);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+enum Kind { MANY, FEW, F32 };
+
+struct Plan {
+  Kind kind;
+  int tile_rows, kb, tiles, parts, part_blocks;
+};
+
+Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, int window, int sinks,
+               size_t ws_bytes) {
+  Plan p;
+  const int group = heads_q / b.n_heads;
+  const long packed = static_cast<long>(m) * group;
+  p.kind = dtype == DT_F32 ? F32 : (packed <= 48l * b.n_seqs ? FEW : MANY);
+  p.tile_rows = p.kind == MANY ? 128 : (p.kind == FEW ? 32 : 16);
+  p.kb = p.kind == MANY ? 64 : (p.kind == FEW ? 32 : 16);
+  p.tiles = static_cast<int>(packed / p.tile_rows) + b.n_seqs;
+  // keys that a tile reads at most
+  long keys = b.max_kv;
+  if (window > 0 && causal)
+    keys = std::min(keys, static_cast<long>(window) + std::min(sinks, b.max_kv) + p.tile_rows / group + 3 * p.kb);
+  const int blocks = static_cast<int>((keys + p.kb - 1) / p.kb);
+  // tiles that there are in earnest, if the rows are spread evenly
+  const long items = std::max<long>(b.n_seqs, (packed + p.tile_rows - 1) / p.tile_rows) * b.n_heads;
+  const long want = p.kind == MANY ? 512 : 2048;         // workgroups to fill the chip
+  const int least = p.kind == MANY ? 4 : (p.kind == FEW ? 8 : 16);  // blocks that are worth one
+  long parts = std::max(1l, std::min<long>((want + items - 1) / items, blocks / least));
+  const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
+  parts = std::max(1l, std::min<long>(parts, static_cast<long>(ws_bytes / per_part)));
+  p.part_blocks = static_cast<int>((blocks + parts - 1) / parts);
+  p.parts = (blocks + p.part_blocks - 1) / p.part_blocks;
+  return p;
+}
+
+size_t plan_bytes(const PagedBatch& b, const Plan& p, int m, int heads_q) {
+  return p.parts == 1 ? 0 : static_cast<size_t>(p.parts) * m * heads_q * (b.d_head + 2) * sizeof(float);
+}
+
+template <int DH>
+void launch_tiles(Kind kind, const AttnArgs& a, dim3 grid, hipStream_t st) {
+  if (kind == F32)
+    hipLaunchKernelGGL(attn_f32<DH>, grid, dim3(64 * kWaves), 0, st, a);
+  else if (kind == FEW)
+    hipLaunchKernelGGL(attn_few<DH>, grid, dim3(64 * kWaves), 0, st, a);
+  else
+    hipLaunchKernelGGL(attn_many<DH>, grid, dim3(64 * kWaves), 0, st, a);
 }
 
 }  // namespace
 
-size_t paged_attention_workspace(int, const PagedBatch&, int, int, int, int) { return 0; }
+size_t paged_attention_workspace(int dtype, const PagedBatch& b, int m, int heads_q, int window, int sinks) {
+  if (m == 0 || b.n_seqs == 0) return 0;
+  const size_t all = ~size_t{0};
+  return std::max(plan_bytes(b, make_plan(dtype, b, m, heads_q, 0, window, sinks, all), m, heads_q),
+                  plan_bytes(b, make_plan(dtype, b, m, heads_q, 1, window, sinks, all), m, heads_q));
+}
 
 hipError_t launch_paged_attention(int dtype, const PagedBatch& b, int m, int heads_q, const void* q, long ld_q,
-                                  bool causal, int window, int sinks, void*, size_t, void* out, long ld_out,
-                                  hipStream_t st) {
+                                  bool causal, int window, int sinks, void* ws, size_t ws_bytes, void* out,
+                                  long ld_out, hipStream_t st) {
   if (m == 0 || b.n_seqs == 0) return hipSuccess;
-  const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(b.d_head));
-  const long grid = static_cast<long>(m) * heads_q;
+  window = std::min(window, kMaxTokens);
+  sinks = std::min(sinks, kMaxTokens);
+  const Plan p = make_plan(dtype, b, m, heads_q, causal, window, sinks, ws_bytes);
+  AttnArgs a{};
+  a.b = b;
+  a.q = q;
+  a.out = out;
+  a.ld_q = ld_q;
+  a.ld_out = ld_out;
+  a.m = m;
+  a.heads_q = heads_q;
+  a.group = heads_q / b.n_heads;
+  a.by_group = make_divisor(a.group);
+  a.causal = causal;
+  a.window = window;
+  a.sinks = window ? sinks : 0;
+  a.scale_log2 = kLog2e / sqrtf(static_cast<float>(b.d_head));
+  a.tile_rows = p.tile_rows;
+  a.tiles = p.tiles;
+  a.parts = p.parts;
+  a.part_blocks = p.part_blocks;
+  if (p.parts > 1) {
+    a.ws_o = static_cast<float*>(ws);
+    a.ws_ml = a.ws_o + static_cast<size_t>(p.parts) * m * heads_q * b.d_head;
+  }
+  const long grid = static_cast<long>(p.tiles) * p.parts * b.n_heads;
   for (long first = 0; first < grid; first += kMaxGrid) {
+    a.first = static_cast<unsigned>(first);
     const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, grid - first)));
+    switch (b.d_head) {
+      case 16: launch_tiles<16>(p.kind, a, part, st); break;
+      case 32: launch_tiles<32>(p.kind, a, part, st); break;
+      case 48: launch_tiles<48>(p.kind, a, part, st); break;
+      case 64: launch_tiles<64>(p.kind, a, part, st); break;
+      case 80: launch_tiles<80>(p.kind, a, part, st); break;
+      case 96: launch_tiles<96>(p.kind, a, part, st); break;
+      case 112: launch_tiles<112>(p.kind, a, part, st); break;
+      case 128: launch_tiles<128>(p.kind, a, part, st); break;
+      default: return hipErrorInvalidValue;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.parts == 1) return hipSuccess;
+  const long rows = static_cast<long>(m) * heads_q;  // below 2^30
+  for (long first = 0; first < rows; first += 4 * kMaxGrid) {
+    a.first = static_cast<unsigned>(first);
+    const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, (rows - first + 3) / 4)));
     if (dtype == DT_BF16)
-      hipLaunchKernelGGL(paged_attn_kernel<bf16_t>, part, dim3(256), 0, st, b, static_cast<const bf16_t*>(q), ld_q,
-                         static_cast<bf16_t*>(out), ld_out, m, heads_q, causal, window, sinks, scale_log2,
-                         static_cast<unsigned>(first));
+      hipLaunchKernelGGL(attn_join<bf16_t>, part, dim3(256), 0, st, a, p.kb);
     else
-      hipLaunchKernelGGL(paged_attn_kernel<float>, part, dim3(256), 0, st, b, static_cast<const float*>(q), ld_q,
-                         static_cast<float*>(out), ld_out, m, heads_q, causal, window, sinks, scale_log2,
-                         static_cast<unsigned>(first));
+      hipLaunchKernelGGL(attn_join<float>, part, dim3(256), 0, st, a, p.kb);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

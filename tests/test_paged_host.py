@@ -136,7 +136,7 @@ def test_rotary_refuses(status, kw):
 
 
 BAD_BATCH = [
-    (SHAPE, dict(d_head=72)), (SHAPE, dict(n_heads=0)), (SHAPE, dict(n_seqs=-1)), (SHAPE, dict(n_seqs=65537)),
+    (SHAPE, dict(d_head=72)), (SHAPE, dict(n_heads=0)), (SHAPE, dict(n_heads=4097)), (SHAPE, dict(n_seqs=-1)), (SHAPE, dict(n_seqs=65537)),
     (SHAPE, dict(page=24)), (SHAPE, dict(page=8)), (SHAPE, dict(page=8192)), (SHAPE, dict(page=0)),
     (SHAPE, dict(page=-16)), (SHAPE, dict(n_pages=0)), (SHAPE, dict(max_pages=0)), (SHAPE, dict(max_kv=65)),
     (SHAPE, dict(max_kv=0)), (SHAPE, dict(max_pages=1 << 27)), (ARG, dict(k=None)), (ARG, dict(v=None)),
