@@ -27,6 +27,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_huge_valf();
+constexpr float kNone = -1e30f;  // maximum of no scores: finite, so that 2^(-inf - kNone) is 0
 constexpr int kWaves = 4;
 constexpr int kGroup = 16;  // keys that always lie in one page
 
@@ -202,7 +203,7 @@ struct Geo {
 template <int DH>
 struct RowState {
   f32x16_t o[Geo<DH>::DT];
-  float m = -kInf;  // reference of the exponents, log2 units
+  float m = kNone;  // reference of the exponents, log2 units
   float l = 0.f;    // this lane's share of the row's sum
   __device__ __forceinline__ RowState() {
 #pragma unroll
@@ -248,62 +249,37 @@ __device__ __forceinline__ void load_values(const bf16_t* vs, int lane, u32x4_t 
       }
 }
 
+// Which of the 64 keys from key0 on the row sees, of those that are alive.
+__device__ __forceinline__ uint64_t first_bits(int n) {
+  return n <= 0 ? 0 : (n >= 64 ? ~uint64_t{0} : (uint64_t{1} << n) - 1);
+}
+__device__ __forceinline__ uint64_t seen_keys(const Row& row, int key0, int sinks, uint64_t alive) {
+  const uint64_t hi = first_bits(row.hi - key0);
+  return hi & (~first_bits(row.lo - key0) | first_bits(sinks - key0)) & alive;
+}
+
 // One block of 32 NSB keys from key0 on, given its scores S^T: mask (unless
 // the whole wave sees the whole block), softmax step, second product.
 // `alive`: a bit per key whose page exists.
-template <int DH, int NSB, bool MASKED>
+template <int DH, int NSB>
 __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NSB], u32x4_t (&vf)[NSB][2][Geo<DH>::DT],
                                              const bf16_t* vs, int key0, const Row& row, int sinks, uint64_t alive,
-                                             float scale_log2) {
+                                             float scale_log2, bool masked) {
   using G = Geo<DH>;
   const int lane = threadIdx.x & 63, hg = lane >> 5;
-  if constexpr (MASKED) {
+  uint64_t odd = 0;  // keys whose value row is not finite throughout
+  if (masked) {
+    const uint64_t seen = seen_keys(row, key0, sinks, alive) >> (4 * hg);
 #pragma unroll
     for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int at = 32 * sb + 8 * (r >> 2) + 4 * hg + (r & 3), key = key0 + at;
-        const bool seen = key < row.hi && (key >= row.lo || key < sinks) && (alive >> at & 1);
-        sc[sb][r] = seen ? sc[sb][r] : -kInf;
-      }
-  }
-  float tmax = -kInf;
-#pragma unroll
-  for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sc[sb][r]);
-  tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-  // p = 2^(s scale - m) for any reference m gives the same softmax, so a row's
-  // reference moves only when its maximum passes it by 2^8: p stays below 256.
-  // The decision is the row's own, the others of the wave multiply by 1.
-  const float m_blk = tmax * scale_log2;
-  const bool grow = m_blk > st.m + 8.f;
-  if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-    const float alpha = grow ? __builtin_amdgcn_exp2f(st.m - m_blk) : 1.f;
-    st.m = grow ? m_blk : st.m;
-    st.l *= alpha;
-#pragma unroll
-    for (int t = 0; t < G::DT; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) st.o[t][r] *= alpha;
-  }
-  const float ref = st.m == -kInf ? 0.f : st.m;  // no key seen yet: every p is 2^-inf
-  float psum = 0.f;
-#pragma unroll
-  for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(sc[sb][r], scale_log2, -ref));
-      sc[sb][r] = p;
-      psum += p;
-    }
-  st.l += psum;
-  uint64_t odd = 0;  // keys whose value row is not finite throughout
-  if constexpr (MASKED) {
+      for (int r = 0; r < 16; ++r)
+        if (!(seen >> (32 * sb + 8 * (r >> 2) + (r & 3)) & 1)) sc[sb][r] = -kInf;
     // 0 times an unseen infinity or NaN would spoil the row: such values leave
-    // the product, and are added to the rows that do see them
+    // the product here, and are added below to the rows that do see them
     bool any = false;
     if (lane < 32 * NSB)
+#pragma unroll 1
       for (int c = 0; c < G::CH; ++c) {
         const u32x4_t x = *reinterpret_cast<const u32x4_t*>(vs + lane * G::ROW + 8 * (c ^ G::v_swizzle(lane)));
 #pragma unroll
@@ -321,36 +297,62 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
             for (int i = 0; i < 4; ++i) vf[sb][s2][t][i] = finite_part(vf[sb][s2][t][i]);
     }
   }
+  float tmax = kNone;
+#pragma unroll
+  for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sc[sb][r]);
+  // p = 2^(s scale - m) for any reference m gives the same softmax, so a row's
+  // reference moves only when its maximum passes it by 2^8: p stays below 256.
+  // The decision is the row's own (either of its lanes'), the other rows of
+  // the wave multiply by 1.
+  if (__builtin_amdgcn_ballot_w64(tmax * scale_log2 > st.m + 8.f) != 0) {
+    const float m_blk = fmaxf(tmax, __shfl_xor(tmax, 32, 64)) * scale_log2;
+    const bool grow = m_blk > st.m + 8.f;
+    const float alpha = grow ? __builtin_amdgcn_exp2f(st.m - m_blk) : 1.f;
+    st.m = grow ? m_blk : st.m;
+    st.l *= alpha;
+#pragma unroll
+    for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[t][r] *= alpha;
+  }
+  float psum = 0.f;
 #pragma unroll
   for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sb][8 * s2 + i], scale_log2, -st.m));
+        psum += p[i];
+      }
       u32x4_t pf;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pf[i] = pack2bf(sc[sb][8 * s2 + 2 * i], sc[sb][8 * s2 + 2 * i + 1]);
+      for (int i = 0; i < 4; ++i) pf[i] = pack2bf(p[2 * i], p[2 * i + 1]);
 #pragma unroll
       for (int t = 0; t < G::DT; ++t)
         st.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[sb][s2][t]),
                                                           __builtin_bit_cast(bf16x8_t, pf), st.o[t], 0, 0, 0);
     }
-  if constexpr (MASKED) {
-    for (odd &= alive; odd; odd &= odd - 1) {
-      const int at = __builtin_ctzll(odd), key = key0 + at;
-      if (!(key < row.hi && (key >= row.lo || key < sinks))) continue;
+  st.l += psum;
+  for (odd &= alive; odd; odd &= odd - 1) {
+    const int at = __builtin_ctzll(odd);
+    if (!(seen_keys(row, key0, sinks, alive) >> at & 1)) continue;
 #pragma unroll
-      for (int t = 0; t < G::DT; ++t)
+    for (int t = 0; t < G::DT; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int d = 32 * t + 8 * j + 4 * hg;
-          const u32x2_t x = *reinterpret_cast<const u32x2_t*>(vs + at * G::ROW + 8 * ((d >> 3) ^ G::v_swizzle(at)) +
-                                                              4 * hg);
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * t + 8 * j + 4 * hg;
+        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(vs + at * G::ROW + 8 * ((d >> 3) ^ G::v_swizzle(at)) +
+                                                            4 * hg);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w = i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16;
-            if ((w & 0x7F800000u) == 0x7F800000u) st.o[t][4 * j + i] += __uint_as_float(w);
-          }
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w = i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16;
+          if ((w & 0x7F800000u) == 0x7F800000u) st.o[t][4 * j + i] += __uint_as_float(w);
         }
-    }
+      }
   }
 }
 
@@ -431,7 +433,7 @@ __device__ __forceinline__ void lds_arrived() {
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 template <int DH>
-__global__ __launch_bounds__(64 * kWaves) void attn_many(const AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_many(const AttnArgs a) {
   using G = Geo<DH>;
   constexpr int KB = 64;                       // keys of a block
   constexpr int RPI = 64 / G::CHP;             // rows that a wave copies at once
@@ -492,32 +494,24 @@ __global__ __launch_bounds__(64 * kWaves) void attn_many(const AttnArgs a) {
     const int key0 = blocks.at(i) * KB;
     if (key0 >= hi_max || (key0 + KB <= lo_min && key0 >= a.sinks)) continue;  // not for this wave
     const bf16_t* kb = ks[buf];
-    u32x4_t kf[2][G::DS];
-#pragma unroll
-    for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-      for (int s = 0; s < G::DS; ++s)
-        kf[sb][s] = *reinterpret_cast<const u32x4_t*>(kb + (32 * sb + c) * G::ROW +
-                                                      8 * ((2 * s + hg) ^ G::k_swizzle(c)));
-    __builtin_amdgcn_sched_barrier(0);
     f32x16_t sc[2];
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb) {
+      u32x4_t kf[G::DS];
+#pragma unroll
+      for (int s = 0; s < G::DS; ++s)
+        kf[s] = *reinterpret_cast<const u32x4_t*>(kb + (32 * sb + c) * G::ROW + 8 * ((2 * s + hg) ^ G::k_swizzle(c)));
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[sb][r] = 0.f;
 #pragma unroll
       for (int s = 0; s < G::DS; ++s)
-        sc[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[sb][s]),
+        sc[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s]),
                                                          __builtin_bit_cast(bf16x8_t, qf[s]), sc[sb], 0, 0, 0);
     }
     u32x4_t vf[2][2][G::DT];
     load_values<DH, 2>(vs[buf], lane, vf);
-    __builtin_amdgcn_sched_barrier(0);
     const bool whole = key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && alive == ~uint64_t{0};
-    if (whole)
-      softmax_step<DH, 2, false>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2);
-    else
-      softmax_step<DH, 2, true>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2);
+    softmax_step<DH, 2>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2, !whole);
   }
   const float l = st.l + __shfl_xor(st.l, 32, 64);
   store_row<DH>(a, row, st, l, hg, part);
@@ -527,7 +521,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_many(const AttnArgs a) {
 // memory to the registers that feed the first product, the values through a
 // piece of LDS of the wave's own; both are loaded a block ahead.
 template <int DH>
-__global__ __launch_bounds__(64 * kWaves) void attn_few(const AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   using G = Geo<DH>;
   constexpr int KB = 32;
   constexpr int RPI = 64 / G::CHP;     // value rows that a wave loads at once
@@ -592,10 +586,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_few(const AttnArgs a) {
     load_values<DH, 1>(vs, lane, vf);
     const bool whole =
         key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && (alive & 0xFFFFFFFFu) == 0xFFFFFFFFu;
-    if (whole)
-      softmax_step<DH, 1, false>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2);
-    else
-      softmax_step<DH, 1, true>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2);
+    softmax_step<DH, 1>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2, !whole);
     wave_order();
   }
   // Join the waves' rows in pairs: the upper half of them leaves maximum, sum
@@ -626,8 +617,8 @@ __global__ __launch_bounds__(64 * kWaves) void attn_few(const AttnArgs a) {
     if (wave < half) {
       const float* o = ol + (wave * 32 + c) * OROW;
       const float m2 = ml[2 * (wave * 32 + c)], l2 = ml[2 * (wave * 32 + c) + 1];
-      const float m_new = fmaxf(st.m, m2), ref = m_new == -kInf ? 0.f : m_new;
-      const float f1 = __builtin_amdgcn_exp2f(st.m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+      const float m_new = fmaxf(st.m, m2);
+      const float f1 = __builtin_amdgcn_exp2f(st.m - m_new), f2 = __builtin_amdgcn_exp2f(m2 - m_new);
       st.m = m_new;
       l = fmaf(l, f1, l2 * f2);
 #pragma unroll
@@ -681,7 +672,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
   f32x4_t acc[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m_run = -kInf, l_run = 0.f;
+  float m_run = kNone, l_run = 0.f;
   PageWindow pages;
   f32x4_t k[DL / 4];
   float v[4][DT];  // V[key 4 g + r][16 t + c]
@@ -728,7 +719,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
         for (int g2 = 0; g2 < 4; ++g2) odd[r] |= (who >> (16 * g2) & 0xFFFF) ? 1u << g2 : 0u;
       }
     }
-    float tmax = -kInf;
+    float tmax = kNone;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int key = key0 + 4 * g + r;
@@ -739,13 +730,12 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
     tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
     tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
     const float m_new = fmaxf(m_run, tmax);
-    const float ref = m_new == -kInf ? 0.f : m_new;
-    const float alpha = exp2f(m_run - ref);
+    const float alpha = exp2f(m_run - m_new);
     m_run = m_new;
     float p[4], psum = 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      p[r] = exp2f(sc[r] - ref);
+      p[r] = exp2f(sc[r] - m_new);
       psum += p[r];
     }
     l_run = fmaf(l_run, alpha, psum);
@@ -791,11 +781,10 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
   float m = part_m[0][i];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w][i]);
-  const float ref = m == -kInf ? 0.f : m;
   float f[kWaves], l = 0.f;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    f[w] = exp2f(part_m[w][i] - ref);
+    f[w] = exp2f(part_m[w][i] - m);
     l = fmaf(part_l[w][i], f[w], l);
   }
   const Row mine = make_row(a, tile, hk, i);
@@ -833,16 +822,15 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb) {
   const int count = tile_blocks(a, t, kb).count;
   const int parts = max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
   const float* ml = a.ws_ml + 2 * item * a.parts;
-  float m = -kInf;
+  float m = kNone;
   for (int p = lane; p < parts; p += 64) m = fmaxf(m, ml[2 * p]);
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const float ref = m == -kInf ? 0.f : m;
   const int dh = a.b.d_head;
   const float* o = a.ws_o + item * a.parts * dh;
   const int d = min(2 * lane, dh - 2);
   float l = 0.f, x = 0.f, y = 0.f;
   for (int p = 0; p < parts; ++p) {
-    const float f = exp2f(ml[2 * p] - ref);
+    const float f = exp2f(ml[2 * p] - m);
     l = fmaf(ml[2 * p + 1], f, l);
     const float2 w = *reinterpret_cast<const float2*>(o + static_cast<long>(p) * dh + d);
     x = fmaf(w.x, f, x);
