@@ -31,14 +31,13 @@ constexpr int kMaxTokens = 1 << 30;  // bound of every token number and of m * h
 struct SeqSpan {
   int row0, n, first, len;
 };
-__device__ __forceinline__ SeqSpan seq_span(const PagedBatch& b, int s, int m) {
+__device__ __forceinline__ SeqSpan seq_span(int start, int end, int kv_len, int max_kv, int m) {
   SeqSpan r;
-  const int start = b.q_start[s], end = b.q_start[s + 1];
   r.row0 = min(max(start, 0), m);
   r.n = max(min(max(end, 0), m) - r.row0, 0);
-  const int len = min(max(b.kv_len[s], 0), kMaxTokens);
+  const int len = min(max(kv_len, 0), kMaxTokens);
   r.first = len - r.n;
-  r.len = min(len, b.max_kv);
+  r.len = min(len, max_kv);
   return r;
 }
 

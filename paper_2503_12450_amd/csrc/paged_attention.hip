@@ -54,34 +54,32 @@ struct Tile {
   int s, r0, n;
 };
 
-// The last sequence with key(s) <= at, where key ascends with s and key(0) = 0:
-// a wave probes 64 places at once.
-template <typename F>
-__device__ __forceinline__ int wave_search(int n_seqs, int at, F&& key) {
+// Tiles are numbered so that sequence s starts at floor(its first packed row /
+// tile_rows) + s: numbers ascend, no two sequences share one, and the few that
+// name no rows end at once.  Needs no pass over the lengths.  A wave finds the
+// sequence of a tile among 64 at a time; with up to 64 that is one round of
+// loads, which brings its rows and length along.
+__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int t) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, n = n_seqs;
-  while (n > 1) {
+  auto first_tile = [&](int s, int start) { return min(max(start, 0), a.m) * a.group / a.tile_rows + s; };
+  int lo = 0, n = a.b.n_seqs;
+  while (n > 64) {
     const int step = (n + 63) >> 6;
-    const int i = lane * step;
-    const bool in = i < n && key(lo + i) <= at;
+    const int i = lo + lane * step;
+    const bool in = lane * step < n && first_tile(i, a.b.q_start[min(i, lo + n - 1)]) <= t;
     const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(in)) - 1, 0);
     lo += k * step;
     n = min(step, n - k * step);
   }
-  return lo;
-}
-
-// Tiles are numbered so that sequence s starts at floor(its first packed row /
-// tile_rows) + s: numbers ascend, no two sequences share one, and the few that
-// name no rows end at once.  Needs no pass over the lengths.
-__device__ __forceinline__ int first_tile(const AttnArgs& a, int s) {
-  return min(max(a.b.q_start[s], 0), a.m) * a.group / a.tile_rows + s;
-}
-__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int t) {
+  const int i = lo + min(lane, n - 1);
+  const int start = a.b.q_start[i], end = a.b.q_start[i + 1], len = a.b.kv_len[i];
+  const bool in = lane < n && first_tile(i, start) <= t;
+  const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(in)) - 1, 0);
   Tile r;
-  r.s = __builtin_amdgcn_readfirstlane(wave_search(a.b.n_seqs, t, [&](int s) { return first_tile(a, s); }));
-  r.sp = seq_span(a.b, r.s, a.m);
-  r.r0 = (t - first_tile(a, r.s)) * a.tile_rows;
+  r.s = __builtin_amdgcn_readfirstlane(lo + k);
+  const int q0 = __builtin_amdgcn_readlane(start, k);
+  r.sp = seq_span(q0, __builtin_amdgcn_readlane(end, k), __builtin_amdgcn_readlane(len, k), a.b.max_kv, a.m);
+  r.r0 = __builtin_amdgcn_readfirstlane((t - first_tile(r.s, q0)) * a.tile_rows);
   r.n = r.r0 < 0 ? 0 : min(a.tile_rows, r.sp.n * a.group - r.r0);
   return r;
 }
@@ -92,23 +90,6 @@ __device__ __forceinline__ int row_hi(const AttnArgs& a, const SeqSpan& sp, int 
 }
 __device__ __forceinline__ int row_lo(const AttnArgs& a, int p) {
   return a.window ? max(0, p - a.window + 1) : 0;
-}
-
-// The blocks of KB keys that a tile reads: blocks 0 .. sink_blocks - 1, then
-// from block0 on, `count` together.
-struct Blocks {
-  int sink_blocks, block0, count;
-  __device__ __forceinline__ int at(int i) const { return i < sink_blocks ? i : block0 + i - sink_blocks; }
-};
-__device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const Tile& t, int kb) {
-  const int p0 = t.sp.first + div_by(t.r0, a.by_group.magic, a.by_group.shift);
-  const int p1 = t.sp.first + div_by(t.r0 + t.n - 1, a.by_group.magic, a.by_group.shift);
-  const int hi = max(row_hi(a, t.sp, p1), 0), lo = row_lo(a, p0);
-  Blocks r;
-  r.block0 = lo / kb;
-  r.sink_blocks = min((min(a.sinks, hi) + kb - 1) / kb, r.block0);
-  r.count = r.sink_blocks + max((hi + kb - 1) / kb - r.block0, 0);
-  return r;
 }
 
 // The pages of 64 consecutive groups of 16 keys, one to a lane, from group 64 *
@@ -132,6 +113,7 @@ struct PageWindow {
   // validity of the n groups from `group` on, a bit per key
   template <int N> __device__ __forceinline__ uint64_t keys(int group) const {
     const uint64_t bits = valid >> (group & 63);
+    if ((bits & ((1u << N) - 1)) == (1u << N) - 1) return N == 4 ? ~uint64_t{0} : (uint64_t{1} << 16 * (N & 3)) - 1;
     uint64_t r = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) r |= (bits >> i & 1) ? uint64_t{0xFFFF} << (16 * i) : 0;
@@ -167,11 +149,34 @@ __device__ __forceinline__ Row make_row(const AttnArgs& a, const Tile& t, int hk
   return r;
 }
 
-__device__ __forceinline__ int wave_min(int v) {
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
+// What rows i .. i + n - 1 of a tile see together: their tokens ascend, so the
+// first and the last row bound both ends.
+struct Reach {
+  int hi_min, hi_max, lo_min, lo_max;  // of no rows: hi_max 0
+};
+__device__ __forceinline__ Reach rows_reach(const AttnArgs& a, const Tile& t, int i, int n) {
+  n = min(n, t.n - i);
+  if (n <= 0) return Reach{0, 0, 0, 0};
+  const int p0 = t.sp.first + div_by(t.r0 + i, a.by_group.magic, a.by_group.shift);
+  const int p1 = t.sp.first + div_by(t.r0 + i + n - 1, a.by_group.magic, a.by_group.shift);
+  return Reach{row_hi(a, t.sp, p0), row_hi(a, t.sp, p1), row_lo(a, p0), row_lo(a, p1)};
 }
-__device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
+
+// The blocks of KB keys that a tile reads: blocks 0 .. sink_blocks - 1, then
+// from block0 on, `count` together.
+struct Blocks {
+  int sink_blocks, block0, count;
+  __device__ __forceinline__ int at(int i) const { return i < sink_blocks ? i : block0 + i - sink_blocks; }
+};
+__device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const Tile& t, int kb) {
+  const Reach reach = rows_reach(a, t, 0, t.n);
+  const int hi = max(reach.hi_max, 0), lo = reach.lo_min;
+  Blocks r;
+  r.block0 = lo / kb;
+  r.sink_blocks = min((min(a.sinks, hi) + kb - 1) / kb, r.block0);
+  r.count = r.sink_blocks + max((hi + kb - 1) / kb - r.block0, 0);
+  return r;
+}
 
 // ---------------------------------------------------------------------------
 // bf16: 32 rows by 32 keys at a time on the 32x32x16 MFMAs, transposed so that
@@ -219,9 +224,9 @@ __device__ __forceinline__ u32x2_t read_tr(const bf16_t* p) {
       u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p)));
 }
 
-__device__ __forceinline__ bool not_finite(uint32_t two) {
-  return (two & 0x7F80u) == 0x7F80u || (two & 0x7F800000u) == 0x7F800000u;
-}
+// Bit 15 (31) of the result is set where the low (high) half of two bf16 is an
+// infinity or NaN: an exponent of all ones carries into it, no other does.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t two) { return (two & 0x7F807F80u) + 0x00800080u; }
 __device__ __forceinline__ uint32_t finite_part(uint32_t two) {
   if ((two & 0x7F80u) == 0x7F80u) two &= 0xFFFF0000u;
   if ((two & 0x7F800000u) == 0x7F800000u) two &= 0xFFFFu;
@@ -277,16 +282,25 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
         if (!(seen >> (32 * sb + 8 * (r >> 2) + (r & 3)) & 1)) sc[sb][r] = -kInf;
     // 0 times an unseen infinity or NaN would spoil the row: such values leave
     // the product here, and are added below to the rows that do see them
-    bool any = false;
-    if (lane < 32 * NSB)
-#pragma unroll 1
-      for (int c = 0; c < G::CH; ++c) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(vs + lane * G::ROW + 8 * (c ^ G::v_swizzle(lane)));
+    uint32_t any = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) any |= not_finite(x[i]);
-      }
-    odd = __builtin_amdgcn_ballot_w64(any);
-    if (odd) {
+    for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int t = 0; t < G::DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) any |= odd_halves(vf[sb][s2][t][i]);
+    if (__builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0) != 0) {
+      any = 0;
+      if (lane < 32 * NSB)
+#pragma unroll 1
+        for (int c = 0; c < G::CH; ++c) {
+          const u32x4_t x = *reinterpret_cast<const u32x4_t*>(vs + lane * G::ROW + 8 * (c ^ G::v_swizzle(lane)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) any |= odd_halves(x[i]);
+        }
+      odd = __builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0);
 #pragma unroll
       for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
@@ -297,46 +311,58 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
             for (int i = 0; i < 4; ++i) vf[sb][s2][t][i] = finite_part(vf[sb][s2][t][i]);
     }
   }
-  float tmax = kNone;
+  // p = 2^(s scale - m) gives the same softmax for any reference m of the row,
+  // as long as nothing overflows: m stays until a lane's p of a block add up to
+  // more than 2^13, and only then (in the first block, and seldom after it) the
+  // maximum is looked for.  Which rows move is their own affair: the others of
+  // the wave multiply by 1 and get the same p again.
+  u32x4_t pf[NSB][2];
+  float psum;
+  auto weights = [&]() {
+    psum = 0.f;
 #pragma unroll
-  for (int sb = 0; sb < NSB; ++sb)
+    for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sc[sb][r]);
-  // p = 2^(s scale - m) for any reference m gives the same softmax, so a row's
-  // reference moves only when its maximum passes it by 2^8: p stays below 256.
-  // The decision is the row's own (either of its lanes'), the other rows of
-  // the wave multiply by 1.
-  if (__builtin_amdgcn_ballot_w64(tmax * scale_log2 > st.m + 8.f) != 0) {
-    const float m_blk = fmaxf(tmax, __shfl_xor(tmax, 32, 64)) * scale_log2;
-    const bool grow = m_blk > st.m + 8.f;
-    const float alpha = grow ? __builtin_amdgcn_exp2f(st.m - m_blk) : 1.f;
-    st.m = grow ? m_blk : st.m;
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float a = __builtin_amdgcn_exp2f(fmaf(sc[sb][8 * s2 + 2 * i], scale_log2, -st.m));
+          const float b = __builtin_amdgcn_exp2f(fmaf(sc[sb][8 * s2 + 2 * i + 1], scale_log2, -st.m));
+          const uint32_t two = pack2bf(a, b);
+          pf[sb][s2][i] = two;
+          // the sum of the weights as rounded: they are what the values are
+          // multiplied by
+          psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, two),
+                                                 __builtin_bit_cast(bf16x2_t, 0x3F803F80u), psum, false);
+        }
+  };
+  weights();
+  if (__builtin_amdgcn_ballot_w64(!(psum <= 8192.f)) != 0) {
+    float top = kNone;
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[sb][r]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale_log2;
+    const bool move = !(fmaxf(psum, __shfl_xor(psum, 32, 64)) <= 8192.f) && top > st.m;
+    const float alpha = move ? __builtin_amdgcn_exp2f(st.m - top) : 1.f;
+    st.m = move ? top : st.m;
     st.l *= alpha;
 #pragma unroll
     for (int t = 0; t < G::DT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[t][r] *= alpha;
+    weights();
   }
-  float psum = 0.f;
+  st.l += psum;
 #pragma unroll
   for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sb][8 * s2 + i], scale_log2, -st.m));
-        psum += p[i];
-      }
-      u32x4_t pf;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) pf[i] = pack2bf(p[2 * i], p[2 * i + 1]);
+    for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
       for (int t = 0; t < G::DT; ++t)
         st.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[sb][s2][t]),
-                                                          __builtin_bit_cast(bf16x8_t, pf), st.o[t], 0, 0, 0);
-    }
-  st.l += psum;
+                                                          __builtin_bit_cast(bf16x8_t, pf[sb][s2]), st.o[t], 0, 0, 0);
   for (odd &= alive; odd; odd &= odd - 1) {
     const int at = __builtin_ctzll(odd);
     if (!(seen_keys(row, key0, sinks, alive) >> at & 1)) continue;
@@ -399,14 +425,16 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Row& row, con
 }
 
 // Work item -> (tile, head, part).  Heads run fastest: workgroups are dealt to
-// the eight XCDs in turn, so the tiles of one head meet in one L2.  Tiles run
-// backwards: with a causal mask the last ones are the longest.
+// the eight XCDs in turn, so the tiles of one head meet in one L2.  Then the
+// tiles, backwards (with a causal mask the last ones are the longest), and the
+// parts slowest: short sequences have the first parts only, which must not all
+// fall to the same XCDs.
 __device__ __forceinline__ void work_item(const AttnArgs& a, int& tile, int& hk, int& part) {
   const unsigned w = a.first + blockIdx.x;
   hk = w % a.b.n_heads;
   const unsigned r = w / a.b.n_heads;
-  part = r % a.parts;
-  tile = a.tiles - 1 - r / a.parts;
+  part = r / a.tiles;
+  tile = a.tiles - 1 - (r - part * a.tiles);
 }
 __device__ __forceinline__ void part_range(const AttnArgs& a, int part, int count, int& from, int& to) {
   from = part * a.part_blocks;
@@ -433,7 +461,7 @@ __device__ __forceinline__ void lds_arrived() {
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 template <int DH>
-__global__ __launch_bounds__(64 * kWaves, 2) void attn_many(const AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const AttnArgs a) {
   using G = Geo<DH>;
   constexpr int KB = 64;                       // keys of a block
   constexpr int RPI = 64 / G::CHP;             // rows that a wave copies at once
@@ -453,9 +481,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_many(const AttnArgs a) {
   const Row row = make_row(a, tile, hk, wave * 32 + c);
   u32x4_t qf[G::DS];
   load_q<DH>(a, row, hg, qf);
-  // what the wave's rows see, for whole blocks
-  const int hi_min = wave_min(row.ok ? row.hi : 0x7FFFFFFF), hi_max = wave_max(row.ok ? row.hi : 0);
-  const int lo_min = wave_min(row.ok ? row.lo : 0x7FFFFFFF), lo_max = wave_max(row.ok ? row.lo : 0);
+  const Reach reach = rows_reach(a, tile, wave * 32, 32);
 
   // The wave copies rows RPI (wave + 4 i) + lane / CHP of a block: they lie in
   // one group of 16 keys, at an offset that depends on the lane alone.
@@ -490,9 +516,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_many(const AttnArgs a) {
     const int buf = (i - from) & 1;
     lds_arrived();  // this block is here, and every wave has left the one before
     const uint64_t alive = alive_next;
-    if (i + 1 < to) copy_block(i + 1, buf ^ 1);
     const int key0 = blocks.at(i) * KB;
-    if (key0 >= hi_max || (key0 + KB <= lo_min && key0 >= a.sinks)) continue;  // not for this wave
+    if (key0 >= reach.hi_max || (key0 + KB <= reach.lo_min && key0 >= a.sinks)) {  // not for this wave
+      if (i + 1 < to) copy_block(i + 1, buf ^ 1);
+      continue;
+    }
     const bf16_t* kb = ks[buf];
     f32x16_t sc[2];
 #pragma unroll
@@ -501,6 +529,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_many(const AttnArgs a) {
 #pragma unroll
       for (int s = 0; s < G::DS; ++s)
         kf[s] = *reinterpret_cast<const u32x4_t*>(kb + (32 * sb + c) * G::ROW + 8 * ((2 * s + hg) ^ G::k_swizzle(c)));
+      // the next block's addresses and copies, while the keys come from LDS
+      if (sb == 0 && i + 1 < to) copy_block(i + 1, buf ^ 1);
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[sb][r] = 0.f;
 #pragma unroll
@@ -510,7 +540,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_many(const AttnArgs a) {
     }
     u32x4_t vf[2][2][G::DT];
     load_values<DH, 2>(vs[buf], lane, vf);
-    const bool whole = key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && alive == ~uint64_t{0};
+    const bool whole =
+        key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && alive == ~uint64_t{0};
     softmax_step<DH, 2>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2, !whole);
   }
   const float l = st.l + __shfl_xor(st.l, 32, 64);
@@ -542,7 +573,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   const Row row = make_row(a, tile, hk, c);
   u32x4_t qf[G::DS];
   load_q<DH>(a, row, hg, qf);
-  const int hi_min = wave_min(row.ok ? row.hi : 0x7FFFFFFF), lo_max = wave_max(row.ok ? row.lo : 0);
+  const Reach reach = rows_reach(a, tile, 0, tile.n);
   bf16_t* vs = reinterpret_cast<bf16_t*>(lds) + wave * KB * G::ROW;
 
   PageWindow pages;
@@ -585,7 +616,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
     u32x4_t vf[1][2][G::DT];
     load_values<DH, 1>(vs, lane, vf);
     const bool whole =
-        key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && (alive & 0xFFFFFFFFu) == 0xFFFFFFFFu;
+        key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && (alive & 0xFFFFFFFFu) == 0xFFFFFFFFu;
     softmax_step<DH, 1>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2, !whole);
     wave_order();
   }
@@ -662,7 +693,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
   part_range(a, part, blocks.count, from, to);
   if (from >= to && from > 0) return;
   const Row row = make_row(a, tile, hk, c);
-  const int hi_min = wave_min(row.ok ? row.hi : 0x7FFFFFFF), lo_max = wave_max(row.ok ? row.lo : 0);
+  const Reach reach = rows_reach(a, tile, 0, tile.n);
   f32x4_t q[DL / 4];
   {
     const float* qr = static_cast<const float*>(a.q) + row.q_at + g * DL;
@@ -700,7 +731,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
     for (int e = 0; e < DL / 4; ++e)
 #pragma unroll
       for (int j = 0; j < 4; ++j) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e][j], q[e][j], sc, 0, 0, 0);
-    const bool whole = key0 + KB <= hi_min && (key0 >= lo_max || key0 + KB <= a.sinks) && alive;
+    const bool whole = key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && alive;
     uint32_t odd[4] = {0, 0, 0, 0};  // [r] bit g: key 4 g + r holds a value that is not finite
     float x[4][DT];
     if (!whole) {
@@ -804,46 +835,66 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// The parts of a row joined: a wave per row, in order of the parts.
+// The parts of a tile's rows joined.  A workgroup takes 32 columns of a few
+// rows: 8 threads read a part's columns, and the 32 such octets divide the rows
+// and their parts, each with a maximum of its own, joined in LDS in order.
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb) {
-  const long item = static_cast<long>(a.first) + static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (item >= static_cast<long>(a.m) * a.heads_q) return;
-  const int row = static_cast<int>(item / a.heads_q), h = static_cast<int>(item - static_cast<long>(row) * a.heads_q);
-  const int lane = threadIdx.x & 63;
-  Tile t;
-  t.s = wave_search(a.b.n_seqs, row, [&](int s) { return a.b.q_start[s]; });
-  t.sp = seq_span(a.b, t.s, a.m);
-  if (row < t.sp.row0 || row >= t.sp.row0 + t.sp.n) return;
-  const int R = (row - t.sp.row0) * a.group + h % a.group;
-  t.r0 = R / a.tile_rows * a.tile_rows;
-  t.n = min(a.tile_rows, t.sp.n * a.group - t.r0);
+__global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int rows) {
+  __shared__ f32x4_t so[256];
+  __shared__ float sm[32], sl[32];
+  const int dh = a.b.d_head, slices = (dh + 31) / 32;
+  unsigned w = a.first + blockIdx.x;
+  const int hk = w % a.b.n_heads;
+  w /= a.b.n_heads;
+  const int d = 32 * (w % slices) + 4 * (threadIdx.x & 7);
+  w /= slices;
+  const int per_tile = (a.tile_rows + rows - 1) / rows;
+  const int row0 = w % per_tile * rows;
+  const Tile t = find_tile(a, w / per_tile);
+  if (row0 >= t.n) return;
   const int count = tile_blocks(a, t, kb).count;
   const int parts = max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
-  const float* ml = a.ws_ml + 2 * item * a.parts;
+  const int octet = threadIdx.x >> 3, subs = 32 / rows;  // octets of a row
+  const int sub = octet % subs;
+  const Row row = make_row(a, t, hk, row0 + octet / subs);
+  const float* ml = a.ws_ml + 2 * row.part * a.parts;
+  const float* o = a.ws_o + row.part * a.parts * dh + min(d, dh - 4);
   float m = kNone;
-  for (int p = lane; p < parts; p += 64) m = fmaxf(m, ml[2 * p]);
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const int dh = a.b.d_head;
-  const float* o = a.ws_o + item * a.parts * dh;
-  const int d = min(2 * lane, dh - 2);
-  float l = 0.f, x = 0.f, y = 0.f;
-  for (int p = 0; p < parts; ++p) {
+  for (int p = sub; p < parts; p += subs) m = fmaxf(m, ml[2 * p]);
+  float l = 0.f;
+  f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int p = sub; p < parts; p += subs) {
+    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(o + static_cast<long>(p) * dh);
     const float f = exp2f(ml[2 * p] - m);
     l = fmaf(ml[2 * p + 1], f, l);
-    const float2 w = *reinterpret_cast<const float2*>(o + static_cast<long>(p) * dh + d);
-    x = fmaf(w.x, f, x);
-    y = fmaf(w.y, f, y);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
+  }
+  so[threadIdx.x] = x;
+  if ((threadIdx.x & 7) == 0) {
+    sm[octet] = m;
+    sl[octet] = l;
+  }
+  __syncthreads();
+  if (sub != 0 || !row.ok || d >= dh) return;
+  for (int k = 1; k < subs; ++k) m = fmaxf(m, sm[octet + k]);
+  x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+  for (int k = 0; k < subs; ++k) {
+    const float f = exp2f(sm[octet + k] - m);
+    l = fmaf(sl[octet + k], f, l);
+    const f32x4_t y = so[threadIdx.x + 8 * k];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  if (2 * lane < dh) {
-    T* out = static_cast<T*>(a.out) + row * a.ld_out + static_cast<long>(h) * dh + d;
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint32_t*>(out) = pack2bf(x * inv, y * inv);
-    else
-      *reinterpret_cast<float2*>(out) = make_float2(x * inv, y * inv);
-  }
+  T* out = static_cast<T*>(a.out) + row.out_at + d;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack2bf(x[0] * inv, x[1] * inv), pack2bf(x[2] * inv, x[3] * inv)};
+  else
+    *reinterpret_cast<f32x4_t*>(out) = f32x4_t{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
 }
 
 // ---------------------------------------------------------------------------
@@ -873,9 +924,11 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   const int blocks = static_cast<int>((keys + p.kb - 1) / p.kb);
   // tiles that there are in earnest, if the rows are spread evenly
   const long items = std::max<long>(b.n_seqs, (packed + p.tile_rows - 1) / p.tile_rows) * b.n_heads;
-  const long want = p.kind == MANY ? 512 : 2048;         // workgroups to fill the chip
-  const int least = p.kind == MANY ? 4 : (p.kind == FEW ? 8 : 16);  // blocks that are worth one
-  long parts = std::max(1l, std::min<long>((want + items - 1) / items, blocks / least));
+  // A workgroup for every CU, if each gets a few blocks; more of them, to even
+  // out sequences of different lengths, as long as each has 1024 keys or more.
+  long parts = std::min<long>((256 + items - 1) / items, blocks / (p.kind == MANY ? 4 : 8));
+  if (p.kind != MANY) parts = std::max(parts, std::min<long>((4096 + items - 1) / items, blocks * p.kb / 1024));
+  parts = std::max(parts, 1l);
   const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
   parts = std::max(1l, std::min<long>(parts, static_cast<long>(ws_bytes / per_part)));
   p.part_blocks = static_cast<int>((blocks + parts - 1) / parts);
@@ -954,14 +1007,17 @@ hipError_t launch_paged_attention(int dtype, const PagedBatch& b, int m, int hea
     if (e != hipSuccess) return e;
   }
   if (p.parts == 1) return hipSuccess;
-  const long rows = static_cast<long>(m) * heads_q;  // below 2^30
-  for (long first = 0; first < rows; first += 4 * kMaxGrid) {
+  // rows of a joining workgroup: about four parts to an octet of threads
+  int rows = 32;
+  while (rows > 1 && rows * p.parts > 128) rows >>= 1;
+  const long joins = static_cast<long>(p.tiles) * ((p.tile_rows + rows - 1) / rows) * ((b.d_head + 31) / 32) * b.n_heads;
+  for (long first = 0; first < joins; first += kMaxGrid) {
     a.first = static_cast<unsigned>(first);
-    const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, (rows - first + 3) / 4)));
+    const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, joins - first)));
     if (dtype == DT_BF16)
-      hipLaunchKernelGGL(attn_join<bf16_t>, part, dim3(256), 0, st, a, p.kb);
+      hipLaunchKernelGGL(attn_join<bf16_t>, part, dim3(256), 0, st, a, p.kb, rows);
     else
-      hipLaunchKernelGGL(attn_join<float>, part, dim3(256), 0, st, a, p.kb);
+      hipLaunchKernelGGL(attn_join<float>, part, dim3(256), 0, st, a, p.kb, rows);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const RowArgs a) {
         lo = right ? lo + half : lo;
         n = right ? n - half : half;
       }
-      const SeqSpan s = seq_span(a.b, lo, a.m);
+      const SeqSpan s = seq_span(a.b.q_start[lo], a.b.q_start[lo + 1], a.b.kv_len[lo], a.b.max_kv, a.m);
       const bool mine = row >= s.row0 && row < s.row0 + s.n;
       const int t = s.first + row - s.row0;
       long at = -1;
