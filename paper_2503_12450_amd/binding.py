@@ -181,9 +181,12 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(stream=None) -> int:
+    if stream is not None:
+        return stream.cuda_stream
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    # the current stream's handle without a Stream object around it (0.3 us
+    # instead of 2.8, of a call that takes 4 to launch a small kernel)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def workspace_bytes(dims) -> int:
@@ -348,25 +351,27 @@ def _refuse(message: str) -> None:
 
 def _dense(name: str, t, dtype, shape, device) -> None:
     """t is a dense tensor of this type and shape (None: any size) on `device`."""
-    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.device != device or not t.is_contiguous():
         _refuse(f"{name}: need a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        _refuse(f"{name}: shape {tuple(t.shape)} is not {shape}")
+    have = t.shape
+    if len(have) != len(shape) or (have != shape and any(n is not None and n != m for n, m in zip(shape, have))):
+        _refuse(f"{name}: shape {tuple(have)} is not {shape}")
 
 
 def _rows(name: str, t, dtype, m: int, d_head: int, device) -> int:
     """t is a matrix of m rows of whole heads on `device`, its columns dense: the
     number of heads."""
-    if t.dtype != dtype or t.device != device:
+    if t.dtype is not dtype or t.device != device:
         _refuse(f"{name}: need a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
-    if t.dim() != 2 or t.shape[0] != m or t.shape[1] % d_head or (t.shape[1] > 1 and t.stride(1) != 1):
-        _refuse(f"{name}: need {m} rows of whole heads of {d_head} dense columns, got {tuple(t.shape)}")
-    return t.shape[1] // d_head
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != m or shape[1] % d_head or (shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"{name}: need {m} rows of whole heads of {d_head} dense columns, got {tuple(shape)}")
+    return shape[1] // d_head
 
 
-def _stride(t) -> int:
+def _stride(t, m: int) -> int:
     """Row stride; a single row has none of its own, so it counts as dense."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if m > 1 else t.shape[1]
 
 
 def _here(device) -> None:
@@ -454,8 +459,8 @@ def k_rotary(rotary: Rotary, x, pos, out, d_head: int, stream=None) -> None:
         _refuse("out and x differ in width")
     _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
     _here(dev)
-    _check(load().mar_k_rotary(_storage_code(x.dtype), ctypes.byref(rotary.c), x.data_ptr(), _stride(x),
-                               pos.data_ptr(), m, heads, d_head, out.data_ptr(), _stride(out), _stream(stream)))
+    _check(load().mar_k_rotary(_storage_code(x.dtype), ctypes.byref(rotary.c), x.data_ptr(), _stride(x, m),
+                               pos.data_ptr(), m, heads, d_head, out.data_ptr(), _stride(out, m), _stream(stream)))
 
 
 def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[Rotary] = None, pos=None,
@@ -472,7 +477,7 @@ def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[
         heads = _rows("q", q, batch.dtype, m, dh, dev)
         if q_out is None or _rows("q_out", q_out, batch.dtype, m, dh, dev) != heads:
             _refuse("q needs a q_out of its width")
-        ldq, ldo = _stride(q), _stride(q_out)
+        ldq, ldo = _stride(q, m), _stride(q_out, m)
     if rotary is not None:
         if pos is None or rotary.freq.device != dev:
             _refuse("rotary needs pos, and its tables on the batch's GPU")
@@ -480,7 +485,7 @@ def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[
     _here(dev)
     _check(load().mar_k_paged_store(batch.code, ctypes.byref(batch.c),
                                     None if rotary is None else ctypes.byref(rotary.c), _ptr(pos), m, k.data_ptr(),
-                                    _stride(k), v.data_ptr(), _stride(v), heads, _ptr(q), ldq,
+                                    _stride(k, m), v.data_ptr(), _stride(v, m), heads, _ptr(q), ldq,
                                     _ptr(q_out) if q is not None else None, ldo, _stream(stream)))
 
 
@@ -509,9 +514,9 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
             _refuse("workspace: need a contiguous tensor on the batch's GPU")
         ws_bytes = workspace.numel() * workspace.element_size()
     _here(dev)
-    _check(load().mar_k_paged_attention(batch.code, ctypes.byref(batch.c), m, heads, q.data_ptr(), _stride(q),
+    _check(load().mar_k_paged_attention(batch.code, ctypes.byref(batch.c), m, heads, q.data_ptr(), _stride(q, m),
                                         1 if causal else 0, window, sinks, _ptr(workspace) if ws_bytes else None,
-                                        ws_bytes, out.data_ptr(), _stride(out), _stream(stream)))
+                                        ws_bytes, out.data_ptr(), _stride(out, m), _stream(stream)))
 
 
 # --------------------------------------------------------------------------

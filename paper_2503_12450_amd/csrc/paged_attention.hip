@@ -943,7 +943,15 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   Plan p;
   const int group = heads_q / b.n_heads;
   const long packed = static_cast<long>(m) * group;
-  p.kind = dtype == DT_F32 ? F32 : (packed <= 48l * b.n_seqs ? FEW : MANY);
+  // Tiles of 32 rows up to 48 rows a sequence, and up to 96 while there are no
+  // more than 512 of them: they spread few rows over more CUs, but read the
+  // keys four times as often as tiles of 128 (2000 keys, 16 heads of 64, 64 rows
+  // in each of 16 sequences: 48 us, tiles of 128: 50; 128 rows: 74 and 55; 32
+  // single tokens and 700 rows together, 4 heads: 40 and 47).
+  const long few = (packed + 31) / 32 * b.n_heads;
+  p.kind = dtype == DT_F32 ? F32
+           : packed <= 48l * b.n_seqs || (packed <= 96l * b.n_seqs && few <= 512) ? FEW
+                                                                                  : MANY;
   p.tile_rows = p.kind == MANY ? 128 : (p.kind == FEW ? 32 : 16);
   p.kb = p.kind == MANY ? 64 : (p.kind == FEW ? 32 : 16);
   p.tiles = static_cast<int>(packed / p.tile_rows) + b.n_seqs;
