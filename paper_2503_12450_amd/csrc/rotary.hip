@@ -28,9 +28,10 @@ struct RowArgs {
   const void *q, *k, *v;
   void* q_out;
   long ld_q, ld_k, ld_v, ld_q_out;
-  int m, heads_q, d_head, rows;  // rows of a workgroup
+  int m, heads_q, d_head;
+  int row_shift;                 // log2 of the rows of a workgroup
   int first;                     // row of workgroup 0
-  Divisor by_units, by_heads;    // d_head / 16 units of a head; heads of a row
+  Divisor by_units;              // d_head / 16 units of a head
 };
 
 __device__ __forceinline__ float2 turn(int pos, double freq) {
@@ -69,74 +70,60 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const RowArgs a) {
   __shared__ float2 cs[kMaxRows * kMaxPairs];
   __shared__ long place[kMaxRows];  // element of the row's first key in the pages, or -1
   __shared__ int owned[kMaxRows];   // the row belongs to a sequence
-  const int row0 = a.first + blockIdx.x * a.rows;
-  const int rows = min(a.rows, a.m - row0);
+  const int row0 = a.first + (blockIdx.x << a.row_shift);
+  const int rows = min(1 << a.row_shift, a.m - row0);
   const int P = a.rot.freq ? a.rot.n_pairs : 0;
-  for (int i = threadIdx.x; i < rows * P; i += kThreads) {
-    const int r = i / P, p = i - r * P;
-    const int ax = a.rot.axis[p];
-    cs[r * kMaxPairs + p] = ax < 0 || ax >= a.rot.n_axes
-                                ? make_float2(1.f, 0.f)
-                                : turn(a.rot.pos[static_cast<long>(row0 + r) * a.rot.n_axes + ax], a.rot.freq[p]);
-  }
-  if constexpr (STORE) {
-    if (threadIdx.x < static_cast<unsigned>(rows)) {
-      const int row = row0 + threadIdx.x;
-      int lo = 0, n = a.b.n_seqs;  // the last sequence that starts at or before the row
-      while (n > 1) {
-        const int half = n >> 1;
-        const bool right = a.b.q_start[lo + half] <= row;
-        lo = right ? lo + half : lo;
-        n = right ? n - half : half;
-      }
-      const SeqSpan s = seq_span(a.b.q_start[lo], a.b.q_start[lo + 1], a.b.kv_len[lo], a.b.max_kv, a.m);
-      const bool mine = row >= s.row0 && row < s.row0 + s.n;
-      const int t = s.first + row - s.row0;
-      long at = -1;
-      if (mine && t >= 0 && t < s.len) {
-        const int page = a.b.table[static_cast<long>(lo) * a.b.max_pages + (t >> a.b.page_shift)];
-        if (page >= 0 && page < a.b.n_pages)
-          at = ((static_cast<long>(page) * a.b.n_heads << a.b.page_shift) + (t & ((1 << a.b.page_shift) - 1))) *
-               a.d_head;
-      }
-      place[threadIdx.x] = at;
-      owned[threadIdx.x] = mine;
-    }
-  }
-  __syncthreads();
   const int units = a.d_head / 16;
   const int heads = a.heads_q + (STORE ? 2 * a.b.n_heads : 0);
-  for (int i = threadIdx.x; i < rows * heads * units; i += kThreads) {
-    const int rh = div_by(i, a.by_units.magic, a.by_units.shift), u = i - rh * units;
-    const int r = div_by(rh, a.by_heads.magic, a.by_heads.shift), h = rh - r * heads;
-    const long row = row0 + r;
-    const T* src;
-    T* dst;
-    bool turned = u < P / 8;
-    if (h < a.heads_q) {
-      if (STORE && !owned[r]) continue;
-      src = static_cast<const T*>(a.q) + row * a.ld_q + h * a.d_head;
-      dst = static_cast<T*>(a.q_out) + row * a.ld_q_out + h * a.d_head;
-    } else {
-      if (place[r] < 0) continue;
-      int hk = h - a.heads_q;
-      const bool value = hk >= a.b.n_heads;
-      if (value) hk -= a.b.n_heads;
-      turned = turned && !value;
-      src = (value ? static_cast<const T*>(a.v) + row * a.ld_v : static_cast<const T*>(a.k) + row * a.ld_k) +
-            hk * a.d_head;
-      dst = static_cast<T*>(value ? a.b.v : a.b.k) + place[r] + (static_cast<long>(hk) * a.d_head << a.b.page_shift);
-    }
+  const int total = heads * units << a.row_shift;
+
+  // Unit i is piece u of head h of row r; rows run faster than heads, so that
+  // the rows of a page's head are written side by side.
+  struct Unit {
+    int r, h, e0, e1, pair;  // pair < 0: not turned
+    bool key, value;
+  };
+  auto unit_of = [&](int i) {
+    Unit t;
+    const int hr = div_by(i, a.by_units.magic, a.by_units.shift), u = i - hr * units;
+    t.h = hr >> a.row_shift;
+    t.r = hr & ((1 << a.row_shift) - 1);
+    t.value = STORE && t.h >= a.heads_q + a.b.n_heads;
+    t.key = STORE && t.h >= a.heads_q && !t.value;
+    const bool turned = u < P / 8 && !t.value;
     const bool halves = turned && !a.rot.neighbours;
-    const int e0 = halves ? 8 * u : 16 * u, e1 = halves ? P + 8 * u : 16 * u + 8;
-    float x[16], y[16];
-    load8(src + e0, x);
-    load8(src + e1, x + 8);
+    t.pair = turned ? 8 * u : -1;
+    t.e0 = halves ? 8 * u : 16 * u;
+    t.e1 = halves ? P + 8 * u : 16 * u + 8;
+    if (t.key) t.h -= a.heads_q;
+    if (t.value) t.h -= a.heads_q + a.b.n_heads;
+    return t;
+  };
+  auto fetch = [&](const Unit& t, float* x) {
+    const long row = row0 + t.r;
+    const T* src = t.value ? static_cast<const T*>(a.v) + row * a.ld_v
+                           : (t.key ? static_cast<const T*>(a.k) + row * a.ld_k
+                                    : static_cast<const T*>(a.q) + row * a.ld_q);
+    src += t.h * a.d_head;
+    load8(src + t.e0, x);
+    load8(src + t.e1, x + 8);
+  };
+  auto finish = [&](const Unit& t, const float* x) {
+    T* dst;
+    if (!t.key && !t.value) {
+      if (STORE && !owned[t.r]) return;
+      dst = static_cast<T*>(a.q_out) + (row0 + t.r) * a.ld_q_out + t.h * a.d_head;
+    } else {
+      if (place[t.r] < 0) return;
+      dst = static_cast<T*>(t.value ? a.b.v : a.b.k) + place[t.r] +
+            (static_cast<long>(t.h) * a.d_head << a.b.page_shift);
+    }
+    float y[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) y[j] = x[j];
-    if (turned) {
-      const float2* c = cs + r * kMaxPairs + 8 * u;
-      if (halves) {
+    if (t.pair >= 0) {
+      const float2* c = cs + t.r * kMaxPairs + t.pair;
+      if (!a.rot.neighbours) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           y[j] = fmaf(x[j], c[j].x, -x[8 + j] * c[j].y);
@@ -150,8 +137,57 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const RowArgs a) {
         }
       }
     }
-    store8(dst + e0, y);
-    store8(dst + e1, y + 8);
+    store8(dst + t.e0, y);
+    store8(dst + t.e1, y + 8);
+  };
+
+  for (int i = threadIdx.x; i < rows * P; i += kThreads) {
+    const int r = i / P, p = i - r * P;
+    const int ax = a.rot.axis[p];
+    cs[r * kMaxPairs + p] = ax < 0 || ax >= a.rot.n_axes
+                                ? make_float2(1.f, 0.f)
+                                : turn(a.rot.pos[static_cast<long>(row0 + r) * a.rot.n_axes + ax], a.rot.freq[p]);
+  }
+  if constexpr (STORE) {
+    // a wave per row finds the last sequence that starts at or before it
+    const int lane = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < rows; r += kThreads / 64) {
+      const int row = row0 + r;
+      int lo = 0, n = a.b.n_seqs;
+      while (n > 64) {
+        const int step = (n + 63) >> 6;
+        const bool in = lane * step < n && a.b.q_start[min(lo + lane * step, lo + n - 1)] <= row;
+        const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(in)) - 1, 0);
+        lo += k * step;
+        n = min(step, n - k * step);
+      }
+      const int i = lo + min(lane, n - 1);
+      const int start = a.b.q_start[i], end = a.b.q_start[i + 1], len = a.b.kv_len[i];
+      const int k = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < n && start <= row)) - 1, 0);
+      const SeqSpan s = seq_span(__builtin_amdgcn_readlane(start, k), __builtin_amdgcn_readlane(end, k),
+                                 __builtin_amdgcn_readlane(len, k), a.b.max_kv, a.m);
+      const bool mine = row >= s.row0 && row < s.row0 + s.n;
+      const int t = s.first + row - s.row0;
+      long at = -1;
+      if (mine && t >= 0 && t < s.len) {
+        const int page = a.b.table[static_cast<long>(lo + k) * a.b.max_pages + (t >> a.b.page_shift)];
+        if (page >= 0 && page < a.b.n_pages)
+          at = ((static_cast<long>(page) * a.b.n_heads << a.b.page_shift) + (t & ((1 << a.b.page_shift) - 1))) *
+               a.d_head;
+      }
+      if (lane == 0) {
+        place[r] = at;
+        owned[r] = mine;
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < total; i += kThreads) {
+    const Unit t = unit_of(i);
+    if (t.r >= rows) continue;
+    float x[16];
+    fetch(t, x);
+    finish(t, x);
   }
 }
 
@@ -159,12 +195,12 @@ template <bool STORE>
 hipError_t launch_rows(int dtype, RowArgs& a, hipStream_t st) {
   const int heads = a.heads_q + (STORE ? 2 * a.b.n_heads : 0);
   if (a.m == 0 || heads == 0 || (STORE && a.b.n_seqs == 0)) return hipSuccess;
-  a.rows = 1;
+  a.row_shift = a.m >= 4096 ? 1 : 0;
   a.by_units = make_divisor(a.d_head / 16);
-  a.by_heads = make_divisor(heads);
-  const long grid = (static_cast<long>(a.m) + a.rows - 1) / a.rows;
+  const int rows = 1 << a.row_shift;
+  const long grid = (static_cast<long>(a.m) + rows - 1) / rows;
   for (long first = 0; first < grid; first += kMaxGrid) {
-    a.first = static_cast<int>(first * a.rows);
+    a.first = static_cast<int>(first * rows);
     const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, grid - first)));
     if (dtype == DT_BF16)
       hipLaunchKernelGGL((rows_kernel<bf16_t, STORE>), part, dim3(kThreads), 0, st, a);
