@@ -699,19 +699,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// fp32: 16 rows; wave w takes blocks w, w + 4, ... of 16 keys, with the fp32
+// fp32: 16 QT rows; wave w takes blocks w, w + 4, ... of 16 keys, with the fp32
 // 16x16x4 MFMAs: S^T (16 keys x 16 rows) = K Q^T, lane (c, g) = (lane % 16,
 // lane / 16) feeding key (row) c at d = g DH/4 + step; O^T (16 d x 16 rows) +=
-// V^T P^T, S^T leaving lane (c, g) with row c's keys 4 g + r.
+// V^T P^T, S^T leaving lane (c, g) with row c's keys 4 g + r.  Keys and values go
+// from L2 to the registers that feed the products, so with many rows the L2
+// bounds: 32 rows to a block of keys instead of 16.
 // ---------------------------------------------------------------------------
-template <int DH>
-__global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
-  constexpr int QB = 16, KB = 16;
+template <int DH, int QT>
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
+  constexpr int KB = 16;
   constexpr int DL = DH / 4;    // floats of a row per lane
   constexpr int DT = DH / 16;   // 16-row tiles of O^T
   constexpr int OROW = DH + 1;
-  __shared__ float part_o[kWaves][QB * OROW];
-  __shared__ float part_m[kWaves][QB], part_l[kWaves][QB];
+  __shared__ float part_o[kWaves][16 * OROW];
+  __shared__ float part_m[kWaves][16], part_l[kWaves][16];
   int tile_no, hk, part;
   work_item(a, tile_no, hk, part);
   const Tile tile = find_tile(a, tile_no);
@@ -722,155 +724,194 @@ __global__ __launch_bounds__(64 * kWaves) void attn_f32(const AttnArgs a) {
   int from, to;
   part_range(a, part, blocks.count, from, to);
   if (from >= to && from > 0) return;
-  const Row row = make_row(a, tile, hk, c);
   const Reach reach = rows_reach(a, tile, 0, tile.n);
-  f32x4_t q[DL / 4];
-  {
+  int row_hi_[QT], row_lo_[QT];
+  f32x4_t q[QT][DL / 4], acc[QT][DT];
+  float m_run[QT], l_run[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const Row row = make_row(a, tile, hk, 16 * qt + c);
+    row_hi_[qt] = row.hi;
+    row_lo_[qt] = row.lo;
     const float* qr = static_cast<const float*>(a.q) + row.q_at + g * DL;
 #pragma unroll
-    for (int i = 0; i < DL / 4; ++i) q[i] = *reinterpret_cast<const f32x4_t*>(qr + 4 * i);
-  }
-  f32x4_t acc[DT];
+    for (int i = 0; i < DL / 4; ++i) q[qt][i] = *reinterpret_cast<const f32x4_t*>(qr + 4 * i);
 #pragma unroll
-  for (int t = 0; t < DT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m_run = kNone, l_run = 0.f;
+    for (int t = 0; t < DT; ++t) acc[qt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m_run[qt] = kNone;
+    l_run[qt] = 0.f;
+  }
   PageWindow pages;
   f32x4_t k[DL / 4];
   float v[4][DT];  // V[key 4 g + r][16 t + c]
   bool alive_next = false;
-  auto load_block = [&](int i) {
+  long at_next = 0;
+  auto seek = [&](int i) {
     const int group = blocks.at(i);
     pages.seek(a.b, tile.s, group);
     alive_next = pages.keys<1>(group) != 0;
-    const long at = key_offset(a.b, pages.page_of(group), hk, group * kGroup, DH);
-    const float* kr = static_cast<const float*>(a.b.k) + at + c * DH + g * DL;
+    at_next = key_offset(a.b, pages.page_of(group), hk, group * kGroup, DH);
+  };
+  auto load_keys = [&]() {
+    const float* kr = static_cast<const float*>(a.b.k) + at_next + c * DH + g * DL;
 #pragma unroll
-    for (int i2 = 0; i2 < DL / 4; ++i2) k[i2] = *reinterpret_cast<const f32x4_t*>(kr + 4 * i2);
-    const float* vr = static_cast<const float*>(a.b.v) + at + 4 * g * DH + c;
+    for (int i = 0; i < DL / 4; ++i) k[i] = *reinterpret_cast<const f32x4_t*>(kr + 4 * i);
+  };
+  auto load_values = [&]() {
+    const float* vr = static_cast<const float*>(a.b.v) + at_next + 4 * g * DH + c;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int t = 0; t < DT; ++t) v[r][t] = vr[r * DH + 16 * t];
   };
-  if (from + wave < to) load_block(from + wave);
+  if (from + wave < to) {
+    seek(from + wave);
+    load_keys();
+    load_values();
+  }
   for (int i = from + wave; i < to; i += kWaves) {
     const int key0 = blocks.at(i) * KB;
-    const bool alive = alive_next;
-    f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+    const bool alive = alive_next, more = i + kWaves < to;
+    const long at = at_next;
+    f32x4_t sc[QT];
 #pragma unroll
-    for (int e = 0; e < DL / 4; ++e)
+    for (int qt = 0; qt < QT; ++qt) {
+      sc[qt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e][j], q[e][j], sc, 0, 0, 0);
+      for (int e = 0; e < DL / 4; ++e)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sc[qt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e][j], q[qt][e][j], sc[qt], 0, 0, 0);
+    }
+    if (more) {
+      seek(i + kWaves);
+      load_keys();
+    }
     const bool whole = key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && alive;
     uint32_t odd[4] = {0, 0, 0, 0};  // [r] bit g: key 4 g + r holds a value that is not finite
-    float x[4][DT];
     if (!whole) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         bool any = false;
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
-          x[r][t] = v[r][t];
           const bool out = !(fabsf(v[r][t]) < kInf);
           any |= out;
-          if (out) v[r][t] = 0.f;
+          v[r][t] = out ? 0.f : v[r][t];
         }
         const uint64_t who = __builtin_amdgcn_ballot_w64(any);
 #pragma unroll
         for (int g2 = 0; g2 < 4; ++g2) odd[r] |= (who >> (16 * g2) & 0xFFFF) ? 1u << g2 : 0u;
       }
     }
-    float tmax = kNone;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int key = key0 + 4 * g + r;
-      const bool seen = whole || (alive && key < row.hi && (key >= row.lo || key < a.sinks));
-      sc[r] = seen ? sc[r] * a.scale_log2 : -kInf;
-      tmax = fmaxf(tmax, sc[r]);
+    for (int qt = 0; qt < QT; ++qt) {
+      float tmax = kNone;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = key0 + 4 * g + r;
+        const bool seen = whole || (alive && key < row_hi_[qt] && (key >= row_lo_[qt] || key < a.sinks));
+        sc[qt][r] = seen ? sc[qt][r] * a.scale_log2 : -kInf;
+        tmax = fmaxf(tmax, sc[qt][r]);
+      }
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+      const float m_new = fmaxf(m_run[qt], tmax);
+      const float alpha = exp2f(m_run[qt] - m_new);
+      m_run[qt] = m_new;
+      float psum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[qt][r] = exp2f(sc[qt][r] - m_new);
+        psum += sc[qt][r];
+      }
+      l_run[qt] = fmaf(l_run[qt], alpha, psum);
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[qt][t][r] *= alpha;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+          acc[qt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][t], sc[qt][r], acc[qt][t], 0, 0, 0);
     }
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-    const float m_new = fmaxf(m_run, tmax);
-    const float alpha = exp2f(m_run - m_new);
-    m_run = m_new;
-    float p[4], psum = 0.f;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      p[r] = exp2f(sc[r] - m_new);
-      psum += p[r];
-    }
-    l_run = fmaf(l_run, alpha, psum);
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) acc[t][r] *= alpha;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int t = 0; t < DT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][t], p[r], acc[t], 0, 0, 0);
     if (!whole && alive) {
       // values that are not finite, for the rows that see their keys
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         for (uint32_t set = odd[r]; set; set &= set - 1) {
-          const int g2 = __builtin_ctz(set), key = key0 + 4 * g2 + r;
-          const bool seen = key < row.hi && (key >= row.lo || key < a.sinks);
+          const int in = 4 * __builtin_ctz(set) + r, key = key0 + in;
+          const float* vr = static_cast<const float*>(a.b.v) + at + in * DH + 4 * g;
 #pragma unroll
-          for (int t = 0; t < DT; ++t)
+          for (int qt = 0; qt < QT; ++qt) {
+            if (!(key < row_hi_[qt] && (key >= row_lo_[qt] || key < a.sinks))) continue;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float y = __shfl(x[r][t], 16 * g2 + 4 * g + e, 64);
-              if (seen && !(fabsf(y) < kInf)) acc[t][e] += y;
-            }
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float y = vr[16 * t + e];
+                if (!(fabsf(y) < kInf)) acc[qt][t][e] += y;
+              }
+          }
         }
     }
-    if (i + kWaves < to) load_block(i + kWaves);
+    if (more) load_values();
   }
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  // Join the waves, 16 rows at a time.
+  for (int qt = 0; qt < QT; ++qt) {
+    if (16 * qt >= tile.n) break;
+    __syncthreads();
 #pragma unroll
-  for (int t = 0; t < DT; ++t)
+    for (int u = 0; u < QT; ++u)
+      if (u == qt) {
+        const float l = l_run[u] + __shfl_xor(l_run[u], 16, 64);
+        const float l4 = l + __shfl_xor(l, 32, 64);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) part_o[wave][c * OROW + 16 * t + 4 * g + r] = acc[t][r];
-  if (g == 0) {
-    part_m[wave][c] = m_run;
-    part_l[wave][c] = l_run;
-  }
-  __syncthreads();
-  const int i = threadIdx.x >> 4;
-  if (i >= tile.n) return;
-  float m = part_m[0][i];
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w][i]);
-  float f[kWaves], l = 0.f;
+          for (int r = 0; r < 4; ++r) part_o[wave][c * OROW + 16 * t + 4 * g + r] = acc[u][t][r];
+        if (g == 0) {
+          part_m[wave][c] = m_run[u];
+          part_l[wave][c] = l4;
+        }
+      }
+    __syncthreads();
+    const int i = threadIdx.x >> 4;
+    if (16 * qt + i >= tile.n) continue;
+    float m = part_m[0][i];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    f[w] = exp2f(part_m[w][i] - m);
-    l = fmaf(part_l[w][i], f[w], l);
-  }
-  const Row mine = make_row(a, tile, hk, i);
-  const bool last = a.parts == 1;
-  const float inv = last ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
-  const long at = mine.part * a.parts + part;
-  float* out = last ? static_cast<float*>(a.out) + mine.out_at : a.ws_o + at * DH;
-  if (!last && (threadIdx.x & 15) == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(m, l);
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w][i]);
+    float f[kWaves], l = 0.f;
 #pragma unroll
-  for (int t = 0; t < DT; ++t) {
-    const int d = 16 * t + (threadIdx.x & 15);
-    float o = 0.f;
+    for (int w = 0; w < kWaves; ++w) {
+      f[w] = exp2f(part_m[w][i] - m);
+      l = fmaf(part_l[w][i], f[w], l);
+    }
+    const Row mine = make_row(a, tile, hk, 16 * qt + i);
+    const bool last = a.parts == 1;
+    const float inv = last ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
+    const long slot = mine.part * a.parts + part;
+    float* out = last ? static_cast<float*>(a.out) + mine.out_at : a.ws_o + slot * DH;
+    if (!last && (threadIdx.x & 15) == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * slot) = make_float2(m, l);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) o = fmaf(part_o[w][i * OROW + d], f[w], o);
-    out[d] = o * inv;
+    for (int t = 0; t < DT; ++t) {
+      const int d = 16 * t + (threadIdx.x & 15);
+      float o = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) o = fmaf(part_o[w][i * OROW + d], f[w], o);
+      out[d] = o * inv;
+    }
   }
 }
 
 // ---------------------------------------------------------------------------
-// The parts of a tile's rows joined.  A workgroup takes 32 columns of a few
-// rows: 8 threads read a part's columns, and the 32 such octets divide the rows
-// and their parts, each with a maximum of its own, joined in LDS in order.
+// The parts of a tile's rows joined.  A workgroup takes 32 columns: 8 threads
+// read a part's columns, and the 32 such octets divide `rows` rows at a time and
+// their parts, each with a maximum of its own, joined in LDS in order.  `shares`
+// workgroups divide a tile's rows.
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int rows) {
+__global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int rows, int shares) {
   __shared__ f32x4_t so[256];
   __shared__ float sm[32], sl[32];
   const int dh = a.b.d_head, slices = (dh + 31) / 32;
@@ -879,52 +920,55 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int r
   w /= a.b.n_heads;
   const int d = 32 * (w % slices) + 4 * (threadIdx.x & 7);
   w /= slices;
-  const int per_tile = (a.tile_rows + rows - 1) / rows;
-  const int row0 = w % per_tile * rows;
-  const Tile t = find_tile(a, w / per_tile);
-  if (row0 >= t.n) return;
+  const int share = w % shares;
+  const Tile t = find_tile(a, w / shares);
+  if (share * rows >= t.n) return;
   const int count = tile_blocks(a, t, kb).count;
   const int parts = max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
   const int octet = threadIdx.x >> 3, subs = 32 / rows;  // octets of a row
   const int sub = octet % subs;
-  const Row row = make_row(a, t, hk, row0 + octet / subs);
-  const float* ml = a.ws_ml + 2 * row.part * a.parts;
-  const float* o = a.ws_o + row.part * a.parts * dh + min(d, dh - 4);
-  float m = kNone;
-  for (int p = sub; p < parts; p += subs) m = fmaxf(m, ml[2 * p]);
-  float l = 0.f;
-  f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+  for (int row0 = share * rows; row0 < t.n; row0 += shares * rows) {
+    const int i = row0 + octet / subs;
+    const Row row = make_row(a, t, hk, i);
+    const float* ml = a.ws_ml + 2 * row.part * a.parts;
+    const float* o = a.ws_o + row.part * a.parts * dh + min(d, dh - 4);
+    float m = kNone;
+    for (int p = sub; p < parts; p += subs) m = fmaxf(m, ml[2 * p]);
+    float l = 0.f;
+    f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int p = sub; p < parts; p += subs) {
-    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(o + static_cast<long>(p) * dh);
-    const float f = exp2f(ml[2 * p] - m);
-    l = fmaf(ml[2 * p + 1], f, l);
+    for (int p = sub; p < parts; p += subs) {
+      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(o + static_cast<long>(p) * dh);
+      const float f = exp2f(ml[2 * p] - m);
+      l = fmaf(ml[2 * p + 1], f, l);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
-  }
-  so[threadIdx.x] = x;
-  if ((threadIdx.x & 7) == 0) {
-    sm[octet] = m;
-    sl[octet] = l;
-  }
-  __syncthreads();
-  if (sub != 0 || !row.ok || d >= dh) return;
-  for (int k = 1; k < subs; ++k) m = fmaxf(m, sm[octet + k]);
-  x = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  l = 0.f;
-  for (int k = 0; k < subs; ++k) {
-    const float f = exp2f(sm[octet + k] - m);
-    l = fmaf(sl[octet + k], f, l);
-    const f32x4_t y = so[threadIdx.x + 8 * k];
+      for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
+    }
+    __syncthreads();  // the rows before are read
+    so[threadIdx.x] = x;
+    if ((threadIdx.x & 7) == 0) {
+      sm[octet] = m;
+      sl[octet] = l;
+    }
+    __syncthreads();
+    if (sub != 0 || i >= t.n || d >= dh) continue;
+    for (int k = 1; k < subs; ++k) m = fmaxf(m, sm[octet + k]);
+    x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+    for (int k = 0; k < subs; ++k) {
+      const float f = exp2f(sm[octet + k] - m);
+      l = fmaf(sl[octet + k], f, l);
+      const f32x4_t y = so[threadIdx.x + 8 * k];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
+      for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    T* out = static_cast<T*>(a.out) + row.out_at + d;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack2bf(x[0] * inv, x[1] * inv), pack2bf(x[2] * inv, x[3] * inv)};
+    else
+      *reinterpret_cast<f32x4_t*>(out) = f32x4_t{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  T* out = static_cast<T*>(a.out) + row.out_at + d;
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack2bf(x[0] * inv, x[1] * inv), pack2bf(x[2] * inv, x[3] * inv)};
-  else
-    *reinterpret_cast<f32x4_t*>(out) = f32x4_t{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
 }
 
 // ---------------------------------------------------------------------------
@@ -952,7 +996,11 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   p.kind = dtype == DT_F32 ? F32
            : packed <= 48l * b.n_seqs || (packed <= 96l * b.n_seqs && few <= 512) ? FEW
                                                                                   : MANY;
-  p.tile_rows = p.kind == MANY ? 128 : (p.kind == FEW ? 32 : 16);
+  // fp32: 32 rows to a tile read the keys half as often, where that still makes
+  // tiles enough (500 rows in each of 4 sequences, 3500 keys, 16 heads of 64: 365
+  // us, tiles of 16: 440; 700 rows in 5 sequences, 12 heads: 25 and 17).
+  const bool wide = packed > 16l * b.n_seqs && few >= 768;
+  p.tile_rows = p.kind == MANY ? 128 : (p.kind == FEW || wide ? 32 : 16);
   p.kb = p.kind == MANY ? 64 : (p.kind == FEW ? 32 : 16);
   p.tiles = static_cast<int>(packed / p.tile_rows) + b.n_seqs;
   // keys that a tile reads at most
@@ -964,7 +1012,10 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   const long items = std::max<long>(b.n_seqs, (packed + p.tile_rows - 1) / p.tile_rows) * b.n_heads;
   // A workgroup for every CU, if each gets a few blocks; more of them, to even
   // out sequences of different lengths, as long as each has 1024 keys or more.
-  long parts = std::min<long>((256 + items - 1) / items, blocks / (p.kind == MANY ? 4 : 8));
+  // (fp32 single tokens: four for every CU; 16 sequences of 3000 tokens, 2 heads
+  // of 128: 34 us, one for every CU: 44.)
+  const long fill = p.kind == F32 && packed <= 16l * b.n_seqs ? 1024 : 256;
+  long parts = std::min<long>((fill + items - 1) / items, blocks / (p.kind == MANY ? 4 : 8));
   if (p.kind != MANY) parts = std::max(parts, std::min<long>((4096 + items - 1) / items, blocks * p.kb / 1024));
   parts = std::max(parts, 1l);
   const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
@@ -980,8 +1031,10 @@ size_t plan_bytes(const PagedBatch& b, const Plan& p, int m, int heads_q) {
 
 template <int DH>
 void launch_tiles(Kind kind, const AttnArgs& a, dim3 grid, hipStream_t st) {
-  if (kind == F32)
-    hipLaunchKernelGGL(attn_f32<DH>, grid, dim3(64 * kWaves), 0, st, a);
+  if (kind == F32 && a.tile_rows == 16)
+    hipLaunchKernelGGL((attn_f32<DH, 1>), grid, dim3(64 * kWaves), 0, st, a);
+  else if (kind == F32)
+    hipLaunchKernelGGL((attn_f32<DH, 2>), grid, dim3(64 * kWaves), 0, st, a);
   else if (kind == FEW)
     hipLaunchKernelGGL(attn_few<DH>, grid, dim3(64 * kWaves), 0, st, a);
   else
@@ -1045,17 +1098,20 @@ hipError_t launch_paged_attention(int dtype, const PagedBatch& b, int m, int hea
     if (e != hipSuccess) return e;
   }
   if (p.parts == 1) return hipSuccess;
-  // rows of a joining workgroup: about four parts to an octet of threads
+  // about four parts to an octet of threads; a tile's rows in turn if there are
+  // enough tiles for every CU, or else a workgroup each
   int rows = 32;
   while (rows > 1 && rows * p.parts > 128) rows >>= 1;
-  const long joins = static_cast<long>(p.tiles) * ((p.tile_rows + rows - 1) / rows) * ((b.d_head + 31) / 32) * b.n_heads;
+  const long each = static_cast<long>(p.tiles) * ((b.d_head + 31) / 32) * b.n_heads;
+  const int shares = each >= 512 ? 1 : std::max(1, p.tile_rows / rows);
+  const long joins = each * shares;
   for (long first = 0; first < joins; first += kMaxGrid) {
     a.first = static_cast<unsigned>(first);
     const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, joins - first)));
     if (dtype == DT_BF16)
-      hipLaunchKernelGGL(attn_join<bf16_t>, part, dim3(256), 0, st, a, p.kb, rows);
+      hipLaunchKernelGGL(attn_join<bf16_t>, part, dim3(256), 0, st, a, p.kb, rows, shares);
     else
-      hipLaunchKernelGGL(attn_join<float>, part, dim3(256), 0, st, a, p.kb, rows);
+      hipLaunchKernelGGL(attn_join<float>, part, dim3(256), 0, st, a, p.kb, rows, shares);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
