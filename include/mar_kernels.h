@@ -183,8 +183,8 @@ mar_status mar_k_rotary(int32_t dtype, const mar_rotary* rotary, const void* x, 
  * * d_head] each, go to their pages; with q given, its n_heads_q heads are
  * rotated into q_out (which may be q itself).  rotary NULL (pos is then
  * ignored): no rotation, keys are stored and queries copied as they are.
- * Strides and alignment as in mar_k_rotary.  Two rows must not name the same
- * place in the cache. */
+ * Strides, alignment and overlaps as in mar_k_rotary; k, v, q and q_out must not
+ * overlap the pages.  Two rows must not name the same place in the cache. */
 mar_status mar_k_paged_store(int32_t dtype, const mar_paged_batch* batch, const mar_rotary* rotary,
                              const int32_t* pos, int32_t m, const void* k, int64_t ld_k, const void* v,
                              int64_t ld_v, int32_t n_heads_q, const void* q, int64_t ld_q, void* q_out,

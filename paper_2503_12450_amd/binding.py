@@ -364,7 +364,7 @@ def _rows(name: str, t, dtype, m: int, d_head: int, device) -> int:
     if t.dtype is not dtype or t.device != device:
         _refuse(f"{name}: need a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
     shape = t.shape
-    if len(shape) != 2 or shape[0] != m or shape[1] % d_head or (shape[1] > 1 and t.stride(1) != 1):
+    if d_head < 1 or len(shape) != 2 or shape[0] != m or shape[1] % d_head or (shape[1] > 1 and t.stride(1) != 1):
         _refuse(f"{name}: need {m} rows of whole heads of {d_head} dense columns, got {tuple(shape)}")
     return shape[1] // d_head
 
@@ -374,17 +374,21 @@ def _stride(t, m: int) -> int:
     return t.stride(0) if m > 1 else t.shape[1]
 
 
-def _here(device) -> None:
+def _stream_here(device, stream) -> int:
+    """The stream's handle; refuses tensors that are not on the current GPU."""
     torch = _torch()
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         _refuse(f"the tensors are on {device}: need the current GPU")
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _storage_code(dtype) -> int:
     torch = _torch()
-    if dtype not in (torch.float32, torch.bfloat16):
+    if dtype is torch.bfloat16:
+        return MAR_BF16
+    if dtype is not torch.float32:
         _refuse(f"unsupported storage type {dtype}")
-    return MAR_F32 if dtype == torch.float32 else MAR_BF16
+    return MAR_F32
 
 
 LAYOUTS = {"halves": MAR_ROTARY_HALVES, "neighbours": MAR_ROTARY_NEIGHBOURS}
@@ -458,9 +462,9 @@ def k_rotary(rotary: Rotary, x, pos, out, d_head: int, stream=None) -> None:
     if _rows("out", out, x.dtype, m, d_head, dev) != heads:
         _refuse("out and x differ in width")
     _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
-    _here(dev)
+    handle = _stream_here(dev, stream)
     _check(load().mar_k_rotary(_storage_code(x.dtype), ctypes.byref(rotary.c), x.data_ptr(), _stride(x, m),
-                               pos.data_ptr(), m, heads, d_head, out.data_ptr(), _stride(out, m), _stream(stream)))
+                               pos.data_ptr(), m, heads, d_head, out.data_ptr(), _stride(out, m), handle))
 
 
 def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[Rotary] = None, pos=None,
@@ -482,16 +486,16 @@ def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[
         if pos is None or rotary.freq.device != dev:
             _refuse("rotary needs pos, and its tables on the batch's GPU")
         _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
-    _here(dev)
+    handle = _stream_here(dev, stream)
     _check(load().mar_k_paged_store(batch.code, ctypes.byref(batch.c),
                                     None if rotary is None else ctypes.byref(rotary.c), _ptr(pos), m, k.data_ptr(),
                                     _stride(k, m), v.data_ptr(), _stride(v, m), heads, _ptr(q), ldq,
-                                    _ptr(q_out) if q is not None else None, ldo, _stream(stream)))
+                                    _ptr(q_out) if q is not None else None, ldo, handle))
 
 
 def paged_attention_workspace_bytes(batch: PagedBatch, m: int, n_heads_q: int, window: int = 0,
                                     sinks: int = 0) -> int:
-    """Bytes of workspace that k_paged_attention makes use of for up to m rows."""
+    """Bytes of workspace that k_paged_attention makes use of for m rows."""
     lib = load()
     n = lib.mar_k_paged_attention_workspace_bytes(batch.code, ctypes.byref(batch.c), m, n_heads_q, window, sinks)
     if n == 0 and lib.mar_last_error():
@@ -513,10 +517,10 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
         if workspace.device != dev or not workspace.is_contiguous():
             _refuse("workspace: need a contiguous tensor on the batch's GPU")
         ws_bytes = workspace.numel() * workspace.element_size()
-    _here(dev)
+    handle = _stream_here(dev, stream)
     _check(load().mar_k_paged_attention(batch.code, ctypes.byref(batch.c), m, heads, q.data_ptr(), _stride(q, m),
                                         1 if causal else 0, window, sinks, _ptr(workspace) if ws_bytes else None,
-                                        ws_bytes, out.data_ptr(), _stride(out, m), _stream(stream)))
+                                        ws_bytes, out.data_ptr(), _stride(out, m), handle))
 
 
 # --------------------------------------------------------------------------

@@ -27,7 +27,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_huge_valf();
-constexpr float kNone = -1e30f;  // maximum of no scores: finite, so that 2^(-inf - kNone) is 0
+constexpr float kNone = -3e38f;  // maximum of no scores: finite, so that 2^(-inf - kNone) is 0
 constexpr int kWaves = 4;
 constexpr int kGroup = 16;  // keys that always lie in one page
 
@@ -353,7 +353,7 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
   // the wave multiply by 1 and get the same p again.
   u32x4_t pf[NSB][2];
   float psum;
-  auto weights = [&]() {
+  auto weights = [&](auto arg) {
     psum = 0.f;
 #pragma unroll
     for (int sb = 0; sb < NSB; ++sb)
@@ -361,9 +361,8 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float a = __builtin_amdgcn_exp2f(fmaf(sc[sb][8 * s2 + 2 * i], scale_log2, -st.m));
-          const float b = __builtin_amdgcn_exp2f(fmaf(sc[sb][8 * s2 + 2 * i + 1], scale_log2, -st.m));
-          const uint32_t two = pack2bf(a, b);
+          const uint32_t two = pack2bf(__builtin_amdgcn_exp2f(arg(sc[sb][8 * s2 + 2 * i])),
+                                       __builtin_amdgcn_exp2f(arg(sc[sb][8 * s2 + 2 * i + 1])));
           pf[sb][s2][i] = two;
           // the sum of the weights as rounded: they are what the values are
           // multiplied by
@@ -371,23 +370,28 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
                                                  __builtin_bit_cast(bf16x2_t, 0x3F803F80u), psum, false);
         }
   };
-  weights();
+  weights([&](float s) { return fmaf(s, scale_log2, -st.m); });
   if (__builtin_amdgcn_ballot_w64(!(psum <= 8192.f)) != 0) {
     float top = kNone;
 #pragma unroll
     for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[sb][r]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale_log2;
-    const bool move = !(fmaxf(psum, __shfl_xor(psum, 32, 64)) <= 8192.f) && top > st.m;
-    const float alpha = move ? __builtin_amdgcn_exp2f(st.m - top) : 1.f;
-    st.m = move ? top : st.m;
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float other = __shfl_xor(psum, 32, 64), m_blk = top * scale_log2;
+    const bool over = !(psum <= 8192.f) || !(other <= 8192.f), move = over && m_blk > st.m;
+    const float alpha = move ? __builtin_amdgcn_exp2f(st.m - m_blk) : 1.f;
+    st.m = move ? m_blk : st.m;
     st.l *= alpha;
 #pragma unroll
     for (int t = 0; t < G::DT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[t][r] *= alpha;
-    weights();
+    // m is rounded, the products below are not: past 2^24 what is between them is
+    // no small exponent any more, and is taken off (smaller scores keep it in
+    // every block alike)
+    const float rest = over && fabsf(st.m) >= 16777216.f ? fmaf(top, scale_log2, -st.m) : 0.f;
+    weights([&](float s) { return fmaf(s, scale_log2, -st.m) - rest; });
   }
   st.l += psum;
 #pragma unroll

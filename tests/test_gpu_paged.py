@@ -117,6 +117,19 @@ def test_rotary_turns_back():
     assert torch.all((back - x).abs() <= 2 * 2 ** 0.5 * 3.5e-7 * r)
 
 
+def test_rotary_of_more_rows_than_one_launch():
+    """2^23 rows and a few: a launch takes 2^22 workgroups of two rows."""
+    m, dh = 2 ** 23 + 5, 16
+    x = torch.zeros((m, dh), dtype=torch.bfloat16, device=DEV)
+    x[:, 0] = 1.0
+    freq, axis = B.rotary_sections((8,), device=DEV)
+    pos = (torch.arange(m, dtype=torch.int32, device=DEV) % 7)[:, None].contiguous()
+    B.k_rotary(B.Rotary(freq, axis, 1), x, pos, x, dh)
+    angle = pos[:, 0].float()
+    assert torch.all((x[:, 0].float() - angle.cos()).abs() <= 2.0 ** -8)
+    assert torch.all((x[:, 8].float() - angle.sin()).abs() <= 2.0 ** -8)
+
+
 # --------------------------------------------------------------------------
 # A cache with batches of ragged sequences
 # --------------------------------------------------------------------------
@@ -288,6 +301,22 @@ def test_attention_scores_of_any_size(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[20, 1], [150, 1]])
+def test_attention_rows_do_not_change_each_other(dtype, rows):
+    """A row whose scores grow from block to block, or are not finite, leaves
+    the bits of the rows that share its wave."""
+    c = Case(64, rows, [400, 500], 2, 1, 64, 16, dtype)
+    before = c.run()
+    c.q[3] *= 400.0
+    c.q[7] = float("nan")
+    c.q[11] = float("inf")
+    after = c.run()
+    rest = [i for i in range(c.m) if i not in (3, 7, 11)]
+    assert torch.equal(before[rest], after[rest])
+    assert not torch.isfinite(after[7]).any() and torch.isfinite(after[3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,kv,heads,kv_heads,window", [
     ([1], [5000], 2, 1, 0), ([1], [5001], 8, 1, 0), ([4, 1], [4097, 3], 4, 2, 0), ([40], [3000], 2, 2, 0),
     ([1, 1, 1], [6000, 1, 700], 2, 1, 0), ([2], [7000], 2, 1, 3000), ([100], [2500], 1, 1, 0),
@@ -362,6 +391,35 @@ def test_attention_many_sequences():
     for dtype in ("bf16", "f32"):
         c = Case(99, rows, kv, 1, 1, 16, 16, dtype, tail=2)
         c.check(c.run(), left=7.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_more_tiles_than_one_launch(dtype):
+    """1100 sequences of one token and 4096 heads: more than 2^22 workgroups.
+    A row's only token is its answer."""
+    n, H, dh = 1100, 4096, 16
+    k = torch.zeros((n, H, 16, dh), dtype=TDT[dtype], device=DEV)
+    v = torch.full_like(k, float("nan"))
+    want = _normal(98, (n, H * dh), dtype)
+    v[:, :, 0] = want.view(n, H, dh)
+    q, out = _normal(99, (n, H * dh), dtype), torch.empty((n, H * dh), dtype=TDT[dtype], device=DEV)
+    i = np.arange(n)
+    batch = B.PagedBatch(B.MarPages(k, v), _i32(i[:, None]), _i32(np.arange(n + 1)), _i32(np.ones(n)))
+    B.k_paged_attention(batch, q, out)
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_attention_scores_near_the_end_of_the_range(dtype, sign):
+    """Every score the same, +-1e30 times an order of magnitude: the mean of the
+    values."""
+    c = Case(63, [3, 70], [100, 90], 1, 1, 32, 16, dtype)
+    c.q.zero_()
+    c.q[:, 0] = 3e18
+    c.k.nan_to_num_(nan=0.0)
+    c.k[..., 0] = sign * 1e15
+    c.check(c.run(False), False)
 
 
 # --------------------------------------------------------------------------

@@ -216,6 +216,7 @@ def test_binding_refuses_what_the_library_cannot_see():
         lambda: B.k_rotary(rot, x, pos[:1], x, 32),                 # rows differ
         lambda: B.k_rotary(rot, x.t(), pos, x.t(), 2),              # columns not dense
         lambda: B.k_rotary(rot, x, pos, x, 48),                     # no whole heads
+        lambda: B.k_rotary(rot, x, pos, x, 0),
         lambda: B.k_rotary(rot, x, pos, x, 32),                     # not on a GPU
         lambda: B.k_paged_store(batch, x, x[:, :32]),               # value heads
         lambda: B.k_paged_store(batch, x.bfloat16(), x.bfloat16()), # not the pages' type
