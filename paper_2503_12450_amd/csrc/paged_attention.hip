@@ -217,19 +217,33 @@ __device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const Tile& t, 
 // second product; V^T follows that order through transposed LDS reads.
 // ---------------------------------------------------------------------------
 
-template <int DH>
+template <int DH_>
 struct Geo {
-  static constexpr int DS = DH / 16;                                // k-steps of S^T
-  static constexpr int DT = (DH + 31) / 32;                         // 32-row tiles of O^T
-  static constexpr int CH = DH / 8;                                 // 16-byte chunks of a row
-  static constexpr int CHP = CH <= 4 ? 4 : (CH <= 8 ? 8 : 16);      // as laid out in LDS
-  static constexpr int ROW = 8 * CHP;                               // elements of a row in LDS
-  // A row's chunk c lies at c ^ swizzle(row), so that the rows that one LDS
-  // access reads fall on different banks: the keys' 16 rows x 1 chunk, the
-  // values' 4 rows x 4 chunks (of 16 chunks, a row of banks).
+  static constexpr int DH = DH_;
+  static constexpr int DS = DH / 16;         // k-steps of S^T
+  static constexpr int DT = (DH + 31) / 32;  // 32-row tiles of O^T
+  static constexpr int CH = DH / 8;          // 16-byte chunks of a row
+};
+// Rows of keys and values in LDS.  A row's chunk c lies at c ^ swizzle(row), so
+// that the rows that one LDS access reads fall on different banks as far as the
+// row length allows: the keys' 16 rows x 1 chunk, the values' 4 rows x 4 chunks
+// (of 16 chunks, a row of banks).
+template <int DH_>
+struct Dense : Geo<DH_> {  // rows without gaps, as the copies leave them
+  using Geo<DH_>::CH;
+  static constexpr int ROW = DH_;
   static __device__ __forceinline__ int k_swizzle(int row) {
-    return CHP == 16 ? row & 15 : (CHP == 8 ? (row >> 1) & 7 : (row >> 2) & 3);
+    return CH == 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : CH % 4 == 0 ? (row >> 2) & 3 : (row >> 3) & 1;
   }
+  static __device__ __forceinline__ int v_swizzle(int row) {
+    return CH == 16 ? (row & 3) << 2 : CH == 8 ? (row >> 1 & 1) << 2 : 0;
+  }
+};
+template <int DH_>
+struct Padded : Geo<DH_> {  // rows of 4, 8 or 16 chunks
+  using Geo<DH_>::CH;
+  static constexpr int CHP = CH <= 4 ? 4 : (CH <= 8 ? 8 : 16);
+  static constexpr int ROW = 8 * CHP;
   static __device__ __forceinline__ int v_swizzle(int row) {
     return CHP == 16 ? (row & 3) << 2 : (CHP == 8 ? (row >> 1 & 1) << 2 : 0);
   }
@@ -266,9 +280,8 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t two) {
 
 // The values' fragments of NSB x 32 keys: element [sb][s2][t] holds keys 32 sb
 // + 16 s2 + {4 h + i, 8 + 4 h + i} of column 32 t + c.
-template <int DH, int NSB>
-__device__ __forceinline__ void load_values(const bf16_t* vs, int lane, u32x4_t (&vf)[NSB][2][Geo<DH>::DT]) {
-  using G = Geo<DH>;
+template <class G, int NSB>
+__device__ __forceinline__ void load_values(const bf16_t* vs, int lane, u32x4_t (&vf)[NSB][2][G::DT]) {
   const int row = 4 * (lane >> 5) + ((lane & 15) >> 2);
   const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   // row's swizzle does not change with the multiples of 8 added to it
@@ -279,7 +292,9 @@ __device__ __forceinline__ void load_values(const bf16_t* vs, int lane, u32x4_t 
     for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
       for (int t = 0; t < G::DT; ++t) {
-        const bf16_t* p = vs + (32 * sb + 16 * s2 + row) * G::ROW + 8 * (((32 * t + col) >> 3) ^ sw) + (col & 7);
+        // columns past the row's end feed rows of O^T that are never stored
+        const int chunk = 32 * t + 32 <= 8 * G::CH ? (32 * t + col) >> 3 : min((32 * t + col) >> 3, G::ROW / 8 - 1);
+        const bf16_t* p = vs + (32 * sb + 16 * s2 + row) * G::ROW + 8 * (chunk ^ sw) + (col & 7);
         const u32x2_t lo = read_tr(p), hi = read_tr(p + 8 * G::ROW);
         vf[sb][s2][t] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
       }
@@ -297,11 +312,10 @@ __device__ __forceinline__ uint64_t seen_keys(const Row& row, int key0, int sink
 // One block of 32 NSB keys from key0 on, given its scores S^T: mask (unless
 // the whole wave sees the whole block), softmax step, second product.
 // `alive`: a bit per key whose page exists.
-template <int DH, int NSB>
-__device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NSB], u32x4_t (&vf)[NSB][2][Geo<DH>::DT],
+template <class G, int NSB>
+__device__ __forceinline__ void softmax_step(RowState<G::DH>& st, f32x16_t (&sc)[NSB], u32x4_t (&vf)[NSB][2][G::DT],
                                              const bf16_t* vs, int key0, const Row& row, int sinks, uint64_t alive,
                                              float scale_log2, bool masked) {
-  using G = Geo<DH>;
   const int lane = threadIdx.x & 63, hg = lane >> 5;
   uint64_t odd = 0;  // keys whose value row is not finite throughout
   if (masked) {
@@ -409,8 +423,8 @@ __device__ __forceinline__ void softmax_step(RowState<DH>& st, f32x16_t (&sc)[NS
     for (int t = 0; t < G::DT; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int d = 32 * t + 8 * j + 4 * hg;
-        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(vs + at * G::ROW + 8 * ((d >> 3) ^ G::v_swizzle(at)) +
+        if (4 * t + j >= G::CH) continue;
+        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(vs + at * G::ROW + 8 * ((4 * t + j) ^ G::v_swizzle(at)) +
                                                             4 * hg);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -491,21 +505,25 @@ __device__ __forceinline__ void copy16(const void* base, int voff, unsigned lds_
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
-// This wave's copies are in LDS and its LDS reads are done; then all waves'.
-__device__ __forceinline__ void lds_arrived() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// All but this wave's last N copies are in LDS and its LDS reads are done; then
+// all waves'.
+template <int N> __device__ __forceinline__ void lds_arrived() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 // LDS operations of one wave execute in order; this keeps the compiler to it.
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-template <int DH>
+// 128 rows, 32 to a wave; the waves share blocks of 64 keys, which lie in a ring
+// in LDS and are copied RING - 1 blocks ahead, a group of 16 keys (of one page)
+// by each wave.  A barrier per block: behind it block i is there for all, and
+// block i - 1's place is free.
+template <int DH, int RING>
 __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const AttnArgs a) {
-  using G = Geo<DH>;
-  constexpr int KB = 64;                       // keys of a block
-  constexpr int RPI = 64 / G::CHP;             // rows that a wave copies at once
-  constexpr int COPIES = KB / (RPI * kWaves);  // times that it does
-  __shared__ __align__(16) bf16_t ks[2][KB * G::ROW];
-  __shared__ __align__(16) bf16_t vs[2][KB * G::ROW];
+  using G = Dense<DH>;
+  constexpr int KB = kWaves * kGroup;
+  constexpr int COPIES = (G::CH + 3) / 4;       // of 64 chunks that make a group of 16 rows
+  constexpr int REST = 16 * G::CH - 64 * (COPIES - 1);  // chunks of the last one
+  __shared__ __align__(256) bf16_t ring[RING][2][KB * G::ROW];
   int tile_no, hk, part;
   work_item(a, tile_no, hk, part);
   const Tile tile = find_tile_longest_first(a, tile_no);
@@ -516,48 +534,56 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
   int from, to;
   part_range(a, part, blocks.count, from, to);
   if (from >= to && from > 0) return;  // attn_join knows which parts there are
+
+  // Byte offsets in the group of the chunks that the lane copies.
+  int koff[COPIES], voff[COPIES];
+#pragma unroll
+  for (int k = 0; k < COPIES; ++k) {
+    const int piece = min(64 * k + lane, 16 * G::CH - 1), r = piece / G::CH, at = piece % G::CH;
+    koff[k] = 2 * (r * DH + 8 * (at ^ G::k_swizzle(r)));
+    voff[k] = 2 * (r * DH + 8 * (at ^ G::v_swizzle(r)));
+  }
+  const unsigned lds0 = static_cast<unsigned>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) bf16_t*)&ring[0][0][kGroup * wave * G::ROW]));
+  PageWindow pages;
+  uint64_t alive[RING];  // of blocks i, i + 1, ... as they are copied
+  auto copy_block = [&](int i) {
+    const int group0 = blocks.at(i) * kWaves, group = group0 + wave;
+    pages.seek(a.b, tile.s, group0);
+    const unsigned lds = lds0 + static_cast<unsigned>(i - from) % RING * (4u * KB * G::ROW);
+    const long at = key_offset(a.b, pages.page_of(group), hk, group * kGroup, DH);
+    const bf16_t* kp = static_cast<const bf16_t*>(a.b.k) + at;
+    const bf16_t* vp = static_cast<const bf16_t*>(a.b.v) + at;
+#pragma unroll
+    for (int k = 0; k < COPIES; ++k)
+      if (k + 1 < COPIES || REST == 64 || lane < REST) {
+        copy16(kp, koff[k], lds + 1024u * k);
+        copy16(vp, voff[k], lds + 1024u * k + 2u * KB * G::ROW);
+      }
+    return pages.keys<kWaves>(group0);
+  };
+#pragma unroll
+  for (int k = 0; k < RING; ++k) alive[k] = k < RING - 1 && from + k < to ? copy_block(from + k) : 0;
+
   const Row row = make_row(a, tile, hk, wave * 32 + c);
   u32x4_t qf[G::DS];
   load_q<DH>(a, row, hg, qf);
   const Reach reach = rows_reach(a, tile, wave * 32, 32);
-
-  // The wave copies rows RPI (wave + 4 i) + lane / CHP of a block: they lie in
-  // one group of 16 keys, at an offset that depends on the lane alone.
-  const int in_group = (RPI * wave) % kGroup + lane / G::CHP;
-  const int copy_row = RPI * wave + lane / G::CHP;  // up to the multiples of 16 that i adds
-  const int chunk = lane % G::CHP;
-  const int koff = 2 * (in_group * DH + 8 * min(chunk ^ G::k_swizzle(copy_row), G::CH - 1));
-  const int voff = 2 * (in_group * DH + 8 * min(chunk ^ G::v_swizzle(copy_row), G::CH - 1));
-  const unsigned ks0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
-      (__attribute__((address_space(3))) bf16_t*)&ks[0][RPI * wave * G::ROW]));
-  const unsigned vs0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(
-      (__attribute__((address_space(3))) bf16_t*)&vs[0][RPI * wave * G::ROW]));
-  PageWindow pages;
-  uint64_t alive_next = 0;
-  auto copy_block = [&](int i, int buf) {
-    const int group0 = blocks.at(i) * (KB / kGroup);
-    pages.seek(a.b, tile.s, group0);
-    alive_next = pages.keys<KB / kGroup>(group0);
-#pragma unroll
-    for (int k = 0; k < COPIES; ++k) {
-      const int group = group0 + RPI * (wave + kWaves * k) / kGroup;
-      const long at = key_offset(a.b, pages.page_of(group), hk, group * kGroup, DH);
-      const unsigned lds = 2u * (buf * KB * G::ROW + RPI * kWaves * k * G::ROW);
-      copy16(static_cast<const bf16_t*>(a.b.k) + at, koff, ks0 + lds);
-      copy16(static_cast<const bf16_t*>(a.b.v) + at, voff, vs0 + lds);
-    }
-  };
-
   RowState<DH> st;
-  if (from < to) copy_block(from, 0);
   for (int i = from; i < to; ++i) {
-    const int buf = (i - from) & 1;
-    lds_arrived();  // this block is here, and every wave has left the one before
-    const uint64_t alive = alive_next;
-    if (i + 1 < to) copy_block(i + 1, buf ^ 1);
+    // of the blocks after i, RING - 2 may still be on their way
+    if (i + RING - 2 < to)
+      lds_arrived<(RING - 2) * 2 * COPIES>();
+    else
+      lds_arrived<0>();
+    if (i + RING - 1 < to) alive[RING - 1] = copy_block(i + RING - 1);
+    const uint64_t here = alive[0];
+#pragma unroll
+    for (int k = 0; k + 1 < RING; ++k) alive[k] = alive[k + 1];
     const int key0 = blocks.at(i) * KB;
     if (key0 >= reach.hi_max || (key0 + KB <= reach.lo_min && key0 >= a.sinks)) continue;  // not for this wave
-    const bf16_t* kb = ks[buf];
+    const bf16_t* kb = ring[static_cast<unsigned>(i - from) % RING][0];
+    const bf16_t* vb = kb + KB * G::ROW;
     f32x16_t sc[2];
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb) {
@@ -573,10 +599,10 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
                                                          __builtin_bit_cast(bf16x8_t, qf[s]), sc[sb], 0, 0, 0);
     }
     u32x4_t vf[2][2][G::DT];
-    load_values<DH, 2>(vs[buf], lane, vf);
+    load_values<G, 2>(vb, lane, vf);
     const bool whole =
-        key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && alive == ~uint64_t{0};
-    softmax_step<DH, 2>(st, sc, vf, vs[buf], key0, row, a.sinks, alive, a.scale_log2, !whole);
+        key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && here == ~uint64_t{0};
+    softmax_step<G, 2>(st, sc, vf, vb, key0, row, a.sinks, here, a.scale_log2, !whole);
   }
   const float l = st.l + __shfl_xor(st.l, 32, 64);
   store_row<DH>(a, row, st, l, hg, part);
@@ -587,7 +613,7 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
 // piece of LDS of the wave's own; both are loaded a block ahead.
 template <int DH>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
-  using G = Geo<DH>;
+  using G = Padded<DH>;
   constexpr int KB = 32;
   constexpr int RPI = 64 / G::CHP;     // value rows that a wave loads at once
   constexpr int LOADS = KB / RPI;
@@ -648,10 +674,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
     if (i + kWaves < to) load_block(i + kWaves);
     wave_order();
     u32x4_t vf[1][2][G::DT];
-    load_values<DH, 1>(vs, lane, vf);
+    load_values<G, 1>(vs, lane, vf);
     const bool whole =
         key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && (alive & 0xFFFFFFFFu) == 0xFFFFFFFFu;
-    softmax_step<DH, 1>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2, !whole);
+    softmax_step<G, 1>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2, !whole);
     wave_order();
   }
   // Join the waves' rows in pairs: the upper half of them leaves maximum, sum
@@ -1042,7 +1068,7 @@ void launch_tiles(Kind kind, const AttnArgs& a, dim3 grid, hipStream_t st) {
   else if (kind == FEW)
     hipLaunchKernelGGL(attn_few<DH>, grid, dim3(64 * kWaves), 0, st, a);
   else
-    hipLaunchKernelGGL(attn_many<DH>, grid, dim3(64 * kWaves), 0, st, a);
+    hipLaunchKernelGGL((attn_many<DH, DH <= 96 ? 3 : 2>), grid, dim3(64 * kWaves), 0, st, a);
 }
 
 }  // namespace
