@@ -12,7 +12,7 @@
 //              (prompts, frames, chunks)
 //   attn_few   32 rows, held by each of four waves, which divide the keys
 //              (single tokens and few rows: bound by reading the cache once)
-//   attn_f32   16 rows on the fp32 MFMAs, the keys divided over the waves
+//   attn_f32   16 or 32 rows on the fp32 MFMAs, the keys divided over the waves
 //
 // Where there are too few tiles to fill the chip, the key blocks of a tile are
 // further divided among workgroups, which leave their rows' maximum, sum and
@@ -1028,7 +1028,7 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
                                                                                   : MANY;
   // fp32: 32 rows to a tile read the keys half as often, where that still makes
   // tiles enough (500 rows in each of 4 sequences, 3500 keys, 16 heads of 64: 365
-  // us, tiles of 16: 440; 700 rows in 5 sequences, 12 heads: 25 and 17).
+  // us, tiles of 16: 440; 377 rows in 5 sequences, 12 heads: 25 and 17).
   const bool wide = packed > 16l * b.n_seqs && few >= 768;
   p.tile_rows = p.kind == MANY ? 128 : (p.kind == FEW || wide ? 32 : 16);
   p.kb = p.kind == MANY ? 64 : (p.kind == FEW ? 32 : 16);
