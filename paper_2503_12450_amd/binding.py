@@ -358,20 +358,16 @@ def _dense(name: str, t, dtype, shape, device) -> None:
         _refuse(f"{name}: shape {tuple(have)} is not {shape}")
 
 
-def _rows(name: str, t, dtype, m: int, d_head: int, device) -> int:
-    """t is a matrix of m rows of whole heads on `device`, its columns dense: the
-    number of heads."""
-    if t.dtype is not dtype or t.device != device:
-        _refuse(f"{name}: need a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
-    shape = t.shape
-    if d_head < 1 or len(shape) != 2 or shape[0] != m or shape[1] % d_head or (shape[1] > 1 and t.stride(1) != 1):
-        _refuse(f"{name}: need {m} rows of whole heads of {d_head} dense columns, got {tuple(shape)}")
-    return shape[1] // d_head
-
-
-def _stride(t, m: int) -> int:
-    """Row stride; a single row has none of its own, so it counts as dense."""
-    return t.stride(0) if m > 1 else t.shape[1]
+def _rows(name: str, t, dtype, m: int, d_head: int, device):
+    """t is a matrix of m rows of whole heads on `device`, its columns dense:
+    (heads, row stride).  A single row has no stride of its own and counts as
+    dense."""
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is dtype and len(shape) == 2 and shape[0] == m and d_head > 0 and not shape[1] % d_head
+            and (stride[1] == 1 or shape[1] == 1) and t.device == device):
+        return shape[1] // d_head, stride[0] if m > 1 else shape[1]
+    _refuse(f"{name}: need {m} rows of whole heads of {d_head} dense columns, {dtype} on {device}, got {tuple(shape)} "
+            f"with strides {stride}, {t.dtype} on {t.device}")
 
 
 def _stream_here(device, stream) -> int:
@@ -419,7 +415,9 @@ class Rotary:
         _dense("freq", freq, torch.float64, (None,), freq.device)
         _dense("axis", axis, torch.int32, (freq.shape[0],), freq.device)
         self.freq, self.axis, self.n_axes = freq, axis, n_axes
+        self.device = freq.device
         self.c = MarRotaryC(freq.data_ptr(), axis.data_ptr(), freq.shape[0], n_axes, LAYOUTS[layout])
+        self.ref = ctypes.byref(self.c)
 
 
 class MarPages:
@@ -446,58 +444,60 @@ class PagedBatch:
         _dense("kv_len", kv_len, torch.int32, (table.shape[0],), dev)
         n_pages, heads, page, d_head = pages.k.shape
         self.pages, self.table, self.q_start, self.kv_len = pages, table, q_start, kv_len
-        self.dtype, self.device, self.d_head = pages.k.dtype, dev, d_head
+        self.dtype, self.device, self.d_head, self.heads = pages.k.dtype, dev, d_head, heads
         self.code = _storage_code(pages.k.dtype)
         self.c = MarPagedBatchC(pages.k.data_ptr(), pages.v.data_ptr(), table.data_ptr(), q_start.data_ptr(),
                                 kv_len.data_ptr(), n_pages, heads, page, d_head, table.shape[0], table.shape[1],
                                 table.shape[1] * page if max_kv is None else max_kv)
+        self.ref = ctypes.byref(self.c)
 
 
 def k_rotary(rotary: Rotary, x, pos, out, d_head: int, stream=None) -> None:
     """out = rotary positions pos [m, n_axes] int32 on the rows of x
     [m, heads * d_head]; out may be x."""
-    torch = _torch()
-    m, dev = x.shape[0], rotary.freq.device
-    heads = _rows("x", x, x.dtype, m, d_head, dev)
-    if _rows("out", out, x.dtype, m, d_head, dev) != heads:
+    m, dev, dtype = x.shape[0], rotary.device, x.dtype
+    heads, ldx = _rows("x", x, dtype, m, d_head, dev)
+    heads_out, ldo = _rows("out", out, dtype, m, d_head, dev)
+    if heads_out != heads:
         _refuse("out and x differ in width")
-    _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
-    handle = _stream_here(dev, stream)
-    _check(load().mar_k_rotary(_storage_code(x.dtype), ctypes.byref(rotary.c), x.data_ptr(), _stride(x, m),
-                               pos.data_ptr(), m, heads, d_head, out.data_ptr(), _stride(out, m), handle))
+    _dense("pos", pos, _torch().int32, (m, rotary.n_axes), dev)
+    _check(load().mar_k_rotary(_storage_code(dtype), rotary.ref, x.data_ptr(), ldx, pos.data_ptr(), m, heads, d_head,
+                               out.data_ptr(), ldo, _stream_here(dev, stream)))
 
 
 def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[Rotary] = None, pos=None,
                   stream=None) -> None:
     """Keys k (rotated) and values v [m, heads * d_head] of the batch's new
     tokens into its pages; q, if given, rotated into q_out (which may be q)."""
-    torch = _torch()
-    m, dev, dh = k.shape[0], batch.device, batch.d_head
-    for name, t in (("k", k), ("v", v)):
-        if _rows(name, t, batch.dtype, m, dh, dev) != batch.c.n_heads:
-            _refuse(f"{name}: need {batch.c.n_heads} heads of {dh}")
+    m, dev, dh, dtype = k.shape[0], batch.device, batch.d_head, batch.dtype
+    heads_k, ldk = _rows("k", k, dtype, m, dh, dev)
+    heads_v, ldv = _rows("v", v, dtype, m, dh, dev)
+    if heads_k != batch.heads or heads_v != batch.heads:
+        _refuse(f"k, v: need {batch.heads} heads of {dh}")
     heads = ldq = ldo = 0
+    q_ptr = out_ptr = rot = pos_ptr = None
     if q is not None:
-        heads = _rows("q", q, batch.dtype, m, dh, dev)
-        if q_out is None or _rows("q_out", q_out, batch.dtype, m, dh, dev) != heads:
-            _refuse("q needs a q_out of its width")
-        ldq, ldo = _stride(q, m), _stride(q_out, m)
+        if q_out is None:
+            _refuse("q needs a q_out")
+        heads, ldq = _rows("q", q, dtype, m, dh, dev)
+        heads_out, ldo = _rows("q_out", q_out, dtype, m, dh, dev)
+        if heads_out != heads:
+            _refuse("q_out and q differ in width")
+        q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     if rotary is not None:
-        if pos is None or rotary.freq.device != dev:
+        if pos is None or rotary.device != dev:
             _refuse("rotary needs pos, and its tables on the batch's GPU")
-        _dense("pos", pos, torch.int32, (m, rotary.n_axes), dev)
-    handle = _stream_here(dev, stream)
-    _check(load().mar_k_paged_store(batch.code, ctypes.byref(batch.c),
-                                    None if rotary is None else ctypes.byref(rotary.c), _ptr(pos), m, k.data_ptr(),
-                                    _stride(k, m), v.data_ptr(), _stride(v, m), heads, _ptr(q), ldq,
-                                    _ptr(q_out) if q is not None else None, ldo, handle))
+        _dense("pos", pos, _torch().int32, (m, rotary.n_axes), dev)
+        rot, pos_ptr = rotary.ref, pos.data_ptr()
+    _check(load().mar_k_paged_store(batch.code, batch.ref, rot, pos_ptr, m, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                    heads, q_ptr, ldq, out_ptr, ldo, _stream_here(dev, stream)))
 
 
 def paged_attention_workspace_bytes(batch: PagedBatch, m: int, n_heads_q: int, window: int = 0,
                                     sinks: int = 0) -> int:
     """Bytes of workspace that k_paged_attention makes use of for m rows."""
     lib = load()
-    n = lib.mar_k_paged_attention_workspace_bytes(batch.code, ctypes.byref(batch.c), m, n_heads_q, window, sinks)
+    n = lib.mar_k_paged_attention_workspace_bytes(batch.code, batch.ref, m, n_heads_q, window, sinks)
     if n == 0 and lib.mar_last_error():
         raise MarError(MAR_E_ARG, lib.mar_last_error().decode())
     return n
@@ -508,19 +508,19 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
     """Attention of the rows q [m, heads * d_head] over their sequences' tokens
     in the pages; workspace: a tensor of any type (see
     paged_attention_workspace_bytes) or None."""
-    m, dev, dh = q.shape[0], batch.device, batch.d_head
-    heads = _rows("q", q, batch.dtype, m, dh, dev)
-    if _rows("out", out, batch.dtype, m, dh, dev) != heads:
+    m, dev, dh, dtype = q.shape[0], batch.device, batch.d_head, batch.dtype
+    heads, ldq = _rows("q", q, dtype, m, dh, dev)
+    heads_out, ldo = _rows("out", out, dtype, m, dh, dev)
+    if heads_out != heads:
         _refuse("out and q differ in width")
-    ws_bytes = 0
+    ws_ptr, ws_bytes = None, 0
     if workspace is not None:
         if workspace.device != dev or not workspace.is_contiguous():
             _refuse("workspace: need a contiguous tensor on the batch's GPU")
         ws_bytes = workspace.numel() * workspace.element_size()
-    handle = _stream_here(dev, stream)
-    _check(load().mar_k_paged_attention(batch.code, ctypes.byref(batch.c), m, heads, q.data_ptr(), _stride(q, m),
-                                        1 if causal else 0, window, sinks, _ptr(workspace) if ws_bytes else None,
-                                        ws_bytes, out.data_ptr(), _stride(out, m), handle))
+        ws_ptr = workspace.data_ptr() if ws_bytes else None
+    _check(load().mar_k_paged_attention(batch.code, batch.ref, m, heads, q.data_ptr(), ldq, 1 if causal else 0, window,
+                                        sinks, ws_ptr, ws_bytes, out.data_ptr(), ldo, _stream_here(dev, stream)))
 
 
 # --------------------------------------------------------------------------
