@@ -1041,12 +1041,16 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   // tiles that there are in earnest, if the rows are spread evenly
   const long items = std::max<long>(b.n_seqs, (packed + p.tile_rows - 1) / p.tile_rows) * b.n_heads;
   // A workgroup for every CU, if each gets a few blocks; more of them, to even
-  // out sequences of different lengths, as long as each has 1024 keys or more.
+  // out sequences of different lengths, as long as each has 1024 keys or more
+  // and there are four or more of them to a tile: the join takes 6 us and more
+  // (64 sequences of 500 to 16000 keys, 15 parts: 137 us, undivided 251; 32 single
+  // tokens and 700 rows on 2100 keys, 2 parts: 33 us, undivided 28).
   // (fp32 single tokens: four for every CU; 16 sequences of 3000 tokens, 2 heads
   // of 128: 34 us, one for every CU: 44.)
   const long fill = p.kind == F32 && packed <= 16l * b.n_seqs ? 1024 : 256;
   long parts = std::min<long>((fill + items - 1) / items, blocks / (p.kind == MANY ? 4 : 8));
-  if (p.kind != MANY) parts = std::max(parts, std::min<long>((4096 + items - 1) / items, blocks * p.kb / 1024));
+  const long even = std::min<long>((4096 + items - 1) / items, static_cast<long>(blocks) * p.kb / 1024);
+  if (p.kind != MANY && even >= 4) parts = std::max(parts, even);
   parts = std::max(parts, 1l);
   const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
   parts = std::max(1l, std::min<long>(parts, static_cast<long>(ws_bytes / per_part)));

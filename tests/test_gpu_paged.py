@@ -347,6 +347,57 @@ def test_attention_max_kv_bounds_the_tokens():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[1, 2], [60, 70]])
+def test_rows_before_the_first_sequence(dtype, rows):
+    """q_start need not begin at row 0."""
+    c = Case(83, rows, [70, 90], 2, 2, 32, 16, dtype, tail=5)
+    c.q_start = (c.q_start + 3).astype(np.int32)
+    c.check(c.run(), left=7.0)
+    k, v = _normal(84, (c.m, 64), dtype), _normal(85, (c.m, 64), dtype)
+    pk, pv = _f64(c.k), _f64(c.v)
+    OP.store(pk, pv, _f64(k).reshape(-1, 2, 32), _f64(v).reshape(-1, 2, 32), c.table, c.q_start, c.kv)
+    B.k_paged_store(c.batch(), k, v)
+    assert np.array_equal(_f64(c.k), pk, equal_nan=True) and np.array_equal(_f64(c.v), pv, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs,m", [(5, 40), (5, 700), (90, 300)])
+def test_nonsense_on_the_device_stays_inside_the_buffers(dtype, seqs, m):
+    """Starts that do not ascend, lengths and tables of any value: what the
+    rows hold is undefined, but nothing around the buffers changes.  (Every index
+    is bounded in the kernels.)"""
+    g = np.random.Generator(np.random.Philox(seqs + m))
+    H, Hk, dh, page, n_pages = 4, 2, 32, 16, 11
+    edge = np.array([-2 ** 31, -1, 0, 1, 5, m - 1, m, m + 1, 2 ** 30, 2 ** 31 - 1])
+    q_start = np.where(g.random(seqs + 1) < 0.5, g.choice(edge, seqs + 1), g.integers(0, m, seqs + 1))
+    kv_len = np.where(g.random(seqs) < 0.5, g.choice(edge, seqs), g.integers(0, 2000, seqs))
+    table = np.where(g.random((seqs, 40)) < 0.3, g.choice(edge, (seqs, 40)), g.integers(0, n_pages, (seqs, 40)))
+
+    def guarded(shape):
+        n = int(np.prod(shape))
+        whole = torch.full((n + 2048,), 7.0, dtype=TDT[dtype], device=DEV)
+        whole[1024:-1024] = _normal(5, (n,), dtype)
+        return whole, whole[1024:-1024].view(shape)
+
+    (wk, k), (wv, v) = guarded((n_pages, Hk, page, dh)), guarded((n_pages, Hk, page, dh))
+    (wo, out), (wq, q_out) = guarded((m, H * dh)), guarded((m, H * dh))
+    batch = B.PagedBatch(B.MarPages(k, v), _i32(table), _i32(q_start), _i32(kv_len))
+    n = B.paged_attention_workspace_bytes(batch, m, H)
+    ws = torch.full((n + 4096,), 0x55, dtype=torch.uint8, device=DEV)
+    q, new = _normal(6, (m, H * dh), dtype), _normal(7, (m, Hk * dh), dtype)
+    freq, axis = B.rotary_sections((16,), device=DEV)
+    pos = torch.zeros((m, 1), dtype=torch.int32, device=DEV)
+    for window in (0, 50):
+        B.k_paged_store(batch, new, new, q, q_out, B.Rotary(freq, axis, 1), pos)
+        B.k_paged_attention(batch, q, out, True, window, 3, ws[:n])
+        B.k_paged_attention(batch, q, out, False, window, 3)
+    torch.cuda.synchronize()
+    for whole in (wk, wv, wo, wq):
+        assert torch.all(whole[:1024] == 7.0) and torch.all(whole[-1024:] == 7.0)
+    assert torch.all(ws[n:] == 0x55)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_on_column_blocks(dtype):
     """q and out as column blocks of wider rows; the other columns stay."""
     c = Case(91, [1, 40], [60, 80], 4, 2, 48, 16, dtype)
@@ -391,6 +442,14 @@ def test_attention_many_sequences():
     for dtype in ("bf16", "f32"):
         c = Case(99, rows, kv, 1, 1, 16, 16, dtype, tail=2)
         c.check(c.run(), left=7.0)
+        k, v = _normal(84, (c.m, 16), dtype), _normal(85, (c.m, 16), dtype)
+        pk, pv = _f64(c.k), _f64(c.v)
+        OP.store(pk, pv, _f64(k).reshape(-1, 1, 16), _f64(v).reshape(-1, 1, 16), c.table, c.q_start, c.kv)
+        B.k_paged_store(c.batch(), k, v)
+        assert np.array_equal(_f64(c.k), pk, equal_nan=True) and np.array_equal(_f64(c.v), pv, equal_nan=True)
+    rows = [int(n) for n in g.integers(90, 150, 70)]   # tiles of 128 rows
+    c = Case(100, rows, [n + int(x) for n, x in zip(rows, g.integers(0, 60, 70))], 1, 1, 16, 16, "bf16", tail=2)
+    c.check(c.run(), left=7.0)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
