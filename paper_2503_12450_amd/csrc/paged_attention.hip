@@ -93,8 +93,8 @@ __device__ __forceinline__ Tile find_tile(const AttnArgs& a, int t) {
 // The same for tiles that are taken whole and in turn: of up to 64 sequences
 // those with the most tokens come first, and the last tiles of a sequence, so
 // that the longest work starts first and the CUs end together (32 sequences of
-// 576 to 1600 tokens, d_head 80, 1024 tiles: 88 us, in the sequences' order
-// 99 us).
+// 578 to 1553 tokens, d_head 80, 1024 tiles: 82 us, in the sequences' order 11
+// more).
 __device__ __forceinline__ Tile find_tile_longest_first(const AttnArgs& a, int t) {
   const int n = a.b.n_seqs;
   if (n > 64) return find_tile(a, a.tiles - 1 - t);
@@ -104,8 +104,8 @@ __device__ __forceinline__ Tile find_tile_longest_first(const AttnArgs& a, int t
   const int tiles = lane < n ? (seq_span(start, end, len, a.b.max_kv, a.m).n * a.group + a.tile_rows - 1) / a.tile_rows : 0;
   int before = 0;  // tiles of the sequences that come before this lane's
   for (int k = 0; k < n; ++k) {
-    const int len_k = __builtin_amdgcn_readlane(len, k);
-    if (len_k > len || (len_k == len && k < lane)) before += __builtin_amdgcn_readlane(tiles, k);
+    const int len_k = __builtin_amdgcn_readlane(len, k), tiles_k = __builtin_amdgcn_readlane(tiles, k);
+    before += (len_k > len) | ((len_k == len) & (k < lane)) ? tiles_k : 0;
   }
   const uint64_t mine = __builtin_amdgcn_ballot_w64(t >= before && t < before + tiles);
   const int s = mine ? __builtin_ctzll(mine) : 0;
@@ -517,6 +517,13 @@ __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_A
 // in LDS and are copied RING - 1 blocks ahead, a group of 16 keys (of one page)
 // by each wave.  A barrier per block: behind it block i is there for all, and
 // block i - 1's place is free.
+// Bound by the vector ALU's part of the softmax (a quarter-rate exp2 per score)
+// and by LDS and memory latency that three waves a SIMD (two above d_head 64)
+// hide in part: 4 chunks of about 1000 rows on 15000 keys, 16 heads of 128 on 4,
+// take 540 us (890 TFLOP/s, matrix units 38 % busy); 31605 rows with a window of
+// 1024, 16 heads of 64: 205 us (660 TFLOP/s, vector ALUs 68 % busy).  Tiles of 256
+// rows (eight waves, or 64 rows to a wave) halve the copies or the LDS reads, but
+// leave fewer waves to hide them and are slower.
 template <int DH, int RING>
 __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const AttnArgs a) {
   using G = Dense<DH>;
@@ -611,6 +618,10 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
 // 32 rows; wave w takes blocks w, w + 4, ... of 32 keys.  The keys go from
 // memory to the registers that feed the first product, the values through a
 // piece of LDS of the wave's own; both are loaded a block ahead.
+// Bound by reading the cache once: 64 sequences of 521 to 15919 keys, 32 query
+// heads of 128 on 4, 579 MB in 130 us (4.5 TB/s); one of 131001, 16 heads on 2,
+// 134 MB in 28 us (4.8 TB/s).  The 32-row products cost nothing there, so single
+// tokens share the form of a few rows.
 template <int DH>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   using G = Padded<DH>;
@@ -734,7 +745,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
 // lane / 16) feeding key (row) c at d = g DH/4 + step; O^T (16 d x 16 rows) +=
 // V^T P^T, S^T leaving lane (c, g) with row c's keys 4 g + r.  Keys and values go
 // from L2 to the registers that feed the products, so with many rows the L2
-// bounds: 32 rows to a block of keys instead of 16.
+// bounds: 32 rows to a block of keys instead of 16 (500 rows in each of 4
+// sequences of 3500 tokens, 16 heads of 64: 352 us, 76 TFLOP/s of 154).
 // ---------------------------------------------------------------------------
 template <int DH, int QT>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
@@ -938,7 +950,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
 // The parts of a tile's rows joined.  A workgroup takes 32 columns: 8 threads
 // read a part's columns, and the 32 such octets divide `rows` rows at a time and
 // their parts, each with a maximum of its own, joined in LDS in order.  `shares`
-// workgroups divide a tile's rows.
+// workgroups divide a tile's rows.  Bound by its launch and three dependent loads:
+// 7 us for 16 rows of 128 parts, 8 us for 2048 rows of up to 15.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int rows, int shares) {

@@ -5,7 +5,11 @@
 // (once per row, shared by all its heads) and the rows' places in the cache go
 // to LDS, then its threads walk the heads in units of 16 elements.  A unit
 // holds 8 whole pairs in either layout, so a thread reads all that it turns
-// before it writes, and the result may overwrite the input.
+// before it writes, and the result may overwrite the input.  40960 rows of 32
+// heads of 64 in bf16 (336 MB) take 65 us, 5.2 TB/s; 17243 rows into pages, 16 + 2
+// x 16 heads of 80 (265 MB), 66 us.  Two rows to a workgroup where there are
+// enough: a page's rows of one head are then written side by side (one row: 73
+// us; four: 68).
 //
 // Angles: pos * freq in fp64, in quarter turns, reduced to [-1/2, 1/2] there
 // and only then rounded to fp32 (positions reach 2^30, where an fp32 angle
