@@ -93,8 +93,8 @@ __device__ __forceinline__ Tile find_tile(const AttnArgs& a, int t) {
 // The same for tiles that are taken whole and in turn: of up to 64 sequences
 // those with the most tokens come first, and the last tiles of a sequence, so
 // that the longest work starts first and the CUs end together (32 sequences of
-// 578 to 1553 tokens, d_head 80, 1024 tiles: 82 us, in the sequences' order 11
-// more).
+// 578 to 1553 tokens, d_head 80, 1024 tiles: 77 us; in the sequences' order it
+// was 11 us more).
 __device__ __forceinline__ Tile find_tile_longest_first(const AttnArgs& a, int t) {
   const int n = a.b.n_seqs;
   if (n > 64) return find_tile(a, a.tiles - 1 - t);
@@ -517,11 +517,16 @@ __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_A
 // in LDS and are copied RING - 1 blocks ahead, a group of 16 keys (of one page)
 // by each wave.  A barrier per block: behind it block i is there for all, and
 // block i - 1's place is free.
+// With two places the next copy is issued right behind that barrier, as it has to
+// arrive by the next one.  With three it has two blocks' time and is issued behind
+// the block's first product, whose LDS reads then do not wait for its addresses
+// (77 against 83 us for 32 frames of 256 rows, 16 heads of 80; with two places
+// that would be 567 against 541 us for the chunks below).
 // Bound by the vector ALU's part of the softmax (a quarter-rate exp2 per score)
 // and by LDS and memory latency that three waves a SIMD (two above d_head 64)
 // hide in part: 4 chunks of about 1000 rows on 15000 keys, 16 heads of 128 on 4,
 // take 540 us (890 TFLOP/s, matrix units 38 % busy); 31605 rows with a window of
-// 1024, 16 heads of 64: 205 us (660 TFLOP/s, vector ALUs 68 % busy).  Tiles of 256
+// 1024, 16 heads of 64: 198 us (690 TFLOP/s, vector ALUs 72 % busy).  Tiles of 256
 // rows (eight waves, or 64 rows to a wave) halve the copies or the LDS reads, but
 // leave fewer waves to hide them and are slower.
 template <int DH, int RING>
@@ -571,6 +576,11 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
   };
 #pragma unroll
   for (int k = 0; k < RING; ++k) alive[k] = k < RING - 1 && from + k < to ? copy_block(from + k) : 0;
+  auto copy_ahead = [&](int i) {
+    if (i + RING - 1 < to) alive[RING - 1] = copy_block(i + RING - 1);
+#pragma unroll
+    for (int k = 0; k + 1 < RING; ++k) alive[k] = alive[k + 1];
+  };
 
   const Row row = make_row(a, tile, hk, wave * 32 + c);
   u32x4_t qf[G::DS];
@@ -583,12 +593,13 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
       lds_arrived<(RING - 2) * 2 * COPIES>();
     else
       lds_arrived<0>();
-    if (i + RING - 1 < to) alive[RING - 1] = copy_block(i + RING - 1);
     const uint64_t here = alive[0];
-#pragma unroll
-    for (int k = 0; k + 1 < RING; ++k) alive[k] = alive[k + 1];
+    if constexpr (RING == 2) copy_ahead(i);
     const int key0 = blocks.at(i) * KB;
-    if (key0 >= reach.hi_max || (key0 + KB <= reach.lo_min && key0 >= a.sinks)) continue;  // not for this wave
+    if (key0 >= reach.hi_max || (key0 + KB <= reach.lo_min && key0 >= a.sinks)) {  // not for this wave
+      if constexpr (RING > 2) copy_ahead(i);
+      continue;
+    }
     const bf16_t* kb = ring[static_cast<unsigned>(i - from) % RING][0];
     const bf16_t* vb = kb + KB * G::ROW;
     f32x16_t sc[2];
@@ -607,6 +618,7 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
     }
     u32x4_t vf[2][2][G::DT];
     load_values<G, 2>(vb, lane, vf);
+    if constexpr (RING > 2) copy_ahead(i);
     const bool whole =
         key0 + KB <= reach.hi_min && (key0 >= reach.lo_max || key0 + KB <= a.sinks) && here == ~uint64_t{0};
     softmax_step<G, 2>(st, sc, vf, vb, key0, row, a.sinks, here, a.scale_log2, !whole);
@@ -767,14 +779,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
   part_range(a, part, blocks.count, from, to);
   if (from >= to && from > 0) return;
   const Reach reach = rows_reach(a, tile, 0, tile.n);
-  int row_hi_[QT], row_lo_[QT];
+  int key_hi[QT], key_lo[QT];
   f32x4_t q[QT][DL / 4], acc[QT][DT];
   float m_run[QT], l_run[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const Row row = make_row(a, tile, hk, 16 * qt + c);
-    row_hi_[qt] = row.hi;
-    row_lo_[qt] = row.lo;
+    key_hi[qt] = row.hi;
+    key_lo[qt] = row.lo;
     const float* qr = static_cast<const float*>(a.q) + row.q_at + g * DL;
 #pragma unroll
     for (int i = 0; i < DL / 4; ++i) q[qt][i] = *reinterpret_cast<const f32x4_t*>(qr + 4 * i);
@@ -851,7 +863,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int key = key0 + 4 * g + r;
-        const bool seen = whole || (alive && key < row_hi_[qt] && (key >= row_lo_[qt] || key < a.sinks));
+        const bool seen = whole || (alive && key < key_hi[qt] && (key >= key_lo[qt] || key < a.sinks));
         sc[qt][r] = seen ? sc[qt][r] * a.scale_log2 : -kInf;
         tmax = fmaxf(tmax, sc[qt][r]);
       }
@@ -886,7 +898,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
           const float* vr = static_cast<const float*>(a.b.v) + at + in * DH + 4 * g;
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
-            if (!(key < row_hi_[qt] && (key >= row_lo_[qt] || key < a.sinks))) continue;
+            if (!(key < key_hi[qt] && (key >= key_lo[qt] || key < a.sinks))) continue;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
