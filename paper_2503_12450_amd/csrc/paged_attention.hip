@@ -493,16 +493,21 @@ __device__ __forceinline__ void part_range(const AttnArgs& a, int part, int coun
   to = part == a.parts - 1 ? count : min(count, from + a.part_blocks);
 }
 
-// Sixteen bytes per lane into LDS at lds_addr + 16 * lane, from a wave-uniform
-// address and a lane's byte offset.  Issued from asm so that the compiler adds
-// no waits of its own; lds_arrived() waits.
+// Twice sixteen bytes per lane into LDS at k_lds (v_lds) + 16 * lane, each from a
+// wave-uniform address and a lane's byte offset.  Issued from asm so that the
+// compiler adds no waits of its own; lds_arrived() waits.  Nor does it add the
+// wait states that the loads need: one after a write of m0, five after a vector
+// instruction that wrote their scalar address (a spilled one comes back that way).
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void copy16(const void* base, int voff, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(lds_addr), "v"(voff), "s"(base)
-               : "memory", "m0");
+__device__ __forceinline__ void copy16(const void* k, int koff, unsigned k_lds, const void* v, int voff,
+                                       unsigned v_lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+      "s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5"
+      :
+      : "s"(k_lds), "v"(koff), "s"(k), "s"(v_lds), "v"(voff), "s"(v)
+      : "memory", "m0");
 }
 #pragma clang diagnostic pop
 // All but this wave's last N copies are in LDS and its LDS reads are done; then
@@ -568,10 +573,8 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
     const bf16_t* vp = static_cast<const bf16_t*>(a.b.v) + at;
 #pragma unroll
     for (int k = 0; k < COPIES; ++k)
-      if (k + 1 < COPIES || REST == 64 || lane < REST) {
-        copy16(kp, koff[k], lds + 1024u * k);
-        copy16(vp, voff[k], lds + 1024u * k + 2u * KB * G::ROW);
-      }
+      if (k + 1 < COPIES || REST == 64 || lane < REST)
+        copy16(kp, koff[k], lds + 1024u * k, vp, voff[k], lds + 1024u * k + 2u * KB * G::ROW);
     return pages.keys<kWaves>(group0);
   };
 #pragma unroll
