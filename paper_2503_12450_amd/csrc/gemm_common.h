@@ -76,6 +76,9 @@ __device__ __forceinline__ i32x4_t make_rsrc(const void* base, unsigned bytes) {
 // with s_waitcnt vmcnt for exactly the slice it is about to read.
 // m0 is reserved by the compiler but nothing else in these kernels uses it
 // (no LDS-DMA builtins, GWS or messages), so clobbering it here is safe.
+// The compiler keeps no wait states inside asm: the load needs one after the
+// write of m0, and five after a vector instruction (v_readfirstlane, or
+// v_readlane for a spilled scalar) that wrote its descriptor or offset.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma16(i32x4_t rsrc, unsigned lds_addr, int voff, int soff) {
@@ -84,7 +87,7 @@ __device__ __forceinline__ void dma16(i32x4_t rsrc, unsigned lds_addr, int voff,
   i32x4_t r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(rsrc[i]);
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
                : "s"(lds_addr), "v"(voff), "s"(r), "s"(soff)
                : "memory", "m0");

@@ -151,3 +151,9 @@ def _check(hazards, pattern):
 
 def test_copies_of_the_paged_attention(hazards):
     _check(hazards, "attn_many")
+
+
+def test_copies_of_every_kernel(hazards):
+    """The products' operand tiles among them."""
+    assert sum("gemm" in name for name, (copies, _) in hazards.items() if copies) > 100
+    _check(hazards, "")
