@@ -15,7 +15,7 @@
 //   attn_f32   16 or 32 rows on the fp32 MFMAs, the keys divided over the waves
 //
 // Where there are too few tiles to fill the chip, the key blocks of a tile are
-// further divided among workgroups, which leave their rows' maximum, sum and
+// further divided among workgroups, which leave their rows' reference, sum and
 // output in the workspace for attn_join.
 #include <algorithm>
 
@@ -27,7 +27,10 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_huge_valf();
-constexpr float kNone = -3e38f;  // maximum of no scores: finite, so that 2^(-inf - kNone) is 0
+// Reference of no scores: finite, so that 2^(-inf - kNone) is 0, and below every
+// finite score, so that the first one overflows against it.
+constexpr float kNone = -3.40282347e38f;
+constexpr float kRough = 4096.f;  // see softmax_step
 constexpr int kWaves = 4;
 constexpr int kGroup = 16;  // keys that always lie in one page
 
@@ -43,7 +46,7 @@ struct AttnArgs {
   int tile_rows;          // packed rows of a tile
   int tiles;              // bound of the tiles of all sequences
   int parts, part_blocks; // workgroups that share a tile, blocks of keys of each
-  float* ws_ml;           // [m * heads_q][parts][2]
+  float* ws_ml;           // [m * heads_q][parts][2]: reference of the exponents, sum
   float* ws_o;            // [m * heads_q][parts][d_head]
   unsigned first;         // work item of workgroup 0
 };
@@ -252,7 +255,7 @@ struct Padded : Geo<DH_> {  // rows of 4, 8 or 16 chunks
 template <int DH>
 struct RowState {
   f32x16_t o[Geo<DH>::DT];
-  float m = kNone;  // reference of the exponents, log2 units
+  float t = kNone;  // the score that the exponents refer to
   float l = 0.f;    // this lane's share of the row's sum
   __device__ __forceinline__ RowState() {
 #pragma unroll
@@ -360,11 +363,16 @@ __device__ __forceinline__ void softmax_step(RowState<G::DH>& st, f32x16_t (&sc)
             for (int i = 0; i < 4; ++i) vf[sb][s2][t][i] = finite_part(vf[sb][s2][t][i]);
     }
   }
-  // p = 2^(s scale - m) gives the same softmax for any reference m of the row,
-  // as long as nothing overflows: m stays until a lane's p of a block add up to
-  // more than 2^13, and only then (in the first block, and seldom after it) the
-  // maximum is looked for.  Which rows move is their own affair: the others of
-  // the wave multiply by 1 and get the same p again.
+  // p = 2^((s - t) scale) gives the same softmax for any reference t of the row, as
+  // long as nothing overflows: t stays until a lane's p of a block add up to more
+  // than 2^13, and only then (in the first block, and seldom after it) the maximum
+  // is looked for.  Which rows move is their own affair: the others of the wave
+  // multiply by 1 and get the same p again.
+  // One FMA gives s scale - m, m = t scale rounded.  What the rounding took, up to
+  // 2^-24 |m|, is the same factor of every p of one t and falls out of their mean;
+  // where references of blocks, waves or parts meet it counts, as little as 2^-13
+  // up to |m| = 2^12.  Rows past that (`rough`) take it off in every block; they
+  // move by their maximum, not by p that lack it.
   u32x4_t pf[NSB][2];
   float psum;
   auto weights = [&](auto arg) {
@@ -384,28 +392,29 @@ __device__ __forceinline__ void softmax_step(RowState<G::DH>& st, f32x16_t (&sc)
                                                  __builtin_bit_cast(bf16x2_t, 0x3F803F80u), psum, false);
         }
   };
-  weights([&](float s) { return fmaf(s, scale_log2, -st.m); });
-  if (__builtin_amdgcn_ballot_w64(!(psum <= 8192.f)) != 0) {
+  const float m = st.t * scale_log2;
+  const bool rough = fabsf(m) >= kRough && st.t != kNone;
+  weights([&](float s) { return fmaf(s, scale_log2, -m); });
+  if (__builtin_amdgcn_ballot_w64(rough || !(psum <= 8192.f)) != 0) {
     float top = kNone;
 #pragma unroll
     for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[sb][r]);
     top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float other = __shfl_xor(psum, 32, 64), m_blk = top * scale_log2;
-    const bool over = !(psum <= 8192.f) || !(other <= 8192.f), move = over && m_blk > st.m;
-    const float alpha = move ? __builtin_amdgcn_exp2f(st.m - m_blk) : 1.f;
-    st.m = move ? m_blk : st.m;
+    const float other = __shfl_xor(psum, 32, 64);
+    const bool over = rough ? (top - st.t) * scale_log2 > 8.f : !(psum <= 8192.f) || !(other <= 8192.f);
+    const bool move = over && top > st.t;
+    const float alpha = move ? __builtin_amdgcn_exp2f((st.t - top) * scale_log2) : 1.f;
+    st.t = move ? top : st.t;
     st.l *= alpha;
 #pragma unroll
     for (int t = 0; t < G::DT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[t][r] *= alpha;
-    // m is rounded, the products below are not: past 2^24 what is between them is
-    // no small exponent any more, and is taken off (smaller scores keep it in
-    // every block alike)
-    const float rest = over && fabsf(st.m) >= 16777216.f ? fmaf(top, scale_log2, -st.m) : 0.f;
-    weights([&](float s) { return fmaf(s, scale_log2, -st.m) - rest; });
+    const float m2 = st.t * scale_log2;
+    const float rest = fabsf(m2) >= kRough && st.t != kNone ? fmaf(st.t, scale_log2, -m2) : 0.f;
+    weights([&](float s) { return fmaf(s, scale_log2, -m2) - rest; });
   }
   st.l += psum;
 #pragma unroll
@@ -451,7 +460,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Row& row, con
   if (!row.ok) return;
   if (a.parts > 1) {
     const long at = row.part * a.parts + part;
-    if (hg == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(st.m, l);
+    if (hg == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(st.t, l);
     float* o = a.ws_o + at * DH;
 #pragma unroll
     for (int t = 0; t < Geo<DH>::DT; ++t)
@@ -706,7 +715,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
     softmax_step<G, 1>(st, sc, vf, vs, key0, row, a.sinks, alive, a.scale_log2, !whole);
     wave_order();
   }
-  // Join the waves' rows in pairs: the upper half of them leaves maximum, sum
+  // Join the waves' rows in pairs: the upper half of them leaves reference, sum
   // and output in LDS, the lower half takes them in.
   float l = st.l + __shfl_xor(st.l, 32, 64);
   float* ol = reinterpret_cast<float*>(lds);
@@ -726,17 +735,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
                 f32x4_t{st.o[t][4 * j], st.o[t][4 * j + 1], st.o[t][4 * j + 2], st.o[t][4 * j + 3]};
         }
       if (hg == 0) {
-        ml[2 * ((wave - half) * 32 + c)] = st.m;
+        ml[2 * ((wave - half) * 32 + c)] = st.t;
         ml[2 * ((wave - half) * 32 + c) + 1] = l;
       }
     }
     __syncthreads();
     if (wave < half) {
       const float* o = ol + (wave * 32 + c) * OROW;
-      const float m2 = ml[2 * (wave * 32 + c)], l2 = ml[2 * (wave * 32 + c) + 1];
-      const float m_new = fmaxf(st.m, m2);
-      const float f1 = __builtin_amdgcn_exp2f(st.m - m_new), f2 = __builtin_amdgcn_exp2f(m2 - m_new);
-      st.m = m_new;
+      const float t2 = ml[2 * (wave * 32 + c)], l2 = ml[2 * (wave * 32 + c) + 1];
+      const float t_new = fmaxf(st.t, t2);
+      const float f1 = __builtin_amdgcn_exp2f((st.t - t_new) * a.scale_log2);
+      const float f2 = __builtin_amdgcn_exp2f((t2 - t_new) * a.scale_log2);
+      st.t = t_new;
       l = fmaf(l, f1, l2 * f2);
 #pragma unroll
       for (int t = 0; t < G::DT; ++t)
@@ -964,7 +974,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
 // ---------------------------------------------------------------------------
 // The parts of a tile's rows joined.  A workgroup takes 32 columns: 8 threads
 // read a part's columns, and the 32 such octets divide `rows` rows at a time and
-// their parts, each with a maximum of its own, joined in LDS in order.  `shares`
+// their parts, each with a reference of its own (bf16: a score; fp32: its scaled
+// maximum, log2 units), joined in LDS in order.  `shares`
 // workgroups divide a tile's rows.  Bound by its launch and three dependent loads:
 // 7 us for 16 rows of 128 parts, 8 us for 2048 rows of up to 15.
 // ---------------------------------------------------------------------------
@@ -972,6 +983,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int rows, int shares) {
   __shared__ f32x4_t so[256];
   __shared__ float sm[32], sl[32];
+  const float unit = sizeof(T) == 2 ? a.scale_log2 : 1.f;
   const int dh = a.b.d_head, slices = (dh + 31) / 32;
   unsigned w = a.first + blockIdx.x;
   const int hk = w % a.b.n_heads;
@@ -997,7 +1009,7 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int r
 #pragma unroll 8
     for (int p = sub; p < parts; p += subs) {
       const f32x4_t y = *reinterpret_cast<const f32x4_t*>(o + static_cast<long>(p) * dh);
-      const float f = exp2f(ml[2 * p] - m);
+      const float f = exp2f((ml[2 * p] - m) * unit);
       l = fmaf(ml[2 * p + 1], f, l);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
@@ -1014,7 +1026,7 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int r
     x = f32x4_t{0.f, 0.f, 0.f, 0.f};
     l = 0.f;
     for (int k = 0; k < subs; ++k) {
-      const float f = exp2f(sm[octet + k] - m);
+      const float f = exp2f((sm[octet + k] - m) * unit);
       l = fmaf(sl[octet + k], f, l);
       const f32x4_t y = so[threadIdx.x + 8 * k];
 #pragma unroll
