@@ -199,7 +199,8 @@ mar_status mar_k_paged_store(int32_t dtype, const mar_paged_batch* batch, const 
  *   (window == 0, or j > p - window, or j < sinks):
  * with a window the last `window` tokens up to its own, and the first `sinks`
  * ones; without `causal` every token after it too.  A row that sees no token
- * becomes zeros; what unseen tokens hold (infinities, NaN) does not matter.
+ * becomes zeros, one whose scores are all -infinity NaN (0 / 0); what unseen
+ * tokens hold (infinities, NaN) does not matter.
  * out must not overlap q or the pages.
  *
  * workspace: device, 16-byte aligned, of mar_k_paged_attention_workspace_bytes

@@ -30,6 +30,9 @@ constexpr float kInf = __builtin_huge_valf();
 // Reference of no scores: finite, so that 2^(-inf - kNone) is 0, and below every
 // finite score, so that the first one overflows against it.
 constexpr float kNone = -3.40282347e38f;
+// The same of a row that saw tokens, all with scores of -infinity: above kNone, so
+// that it stays where waves and parts are joined by the larger reference.
+constexpr float kOnlyInf = -3.40282326e38f;
 constexpr float kRough = 4096.f;  // see softmax_step
 constexpr int kWaves = 4;
 constexpr int kGroup = 16;  // keys that always lie in one page
@@ -444,6 +447,29 @@ __device__ __forceinline__ void softmax_step(RowState<G::DH>& st, f32x16_t (&sc)
   }
 }
 
+// 1 / l.  A row without weights: zeros if it sees no token; 0 / 0 if it sees some
+// and every score is -infinity.
+__device__ __forceinline__ float inverse_sum(float l, float ref) {
+  return l != 0.f ? 1.0f / l : (ref == kNone ? 0.f : __builtin_nanf(""));
+}
+
+// Reference `ref` of a row of which blocks from, from + step, ... < to left the sum
+// l: tells apart whether one without weights saw a token.  Reads the table again,
+// in the waves that have such rows.
+template <int KB>
+__device__ __forceinline__ float mark_seen(const AttnArgs& a, int s, const Blocks& blocks, int from, int to, int step,
+                                           const Row& row, float l, PageWindow& pages, float ref) {
+  const bool empty = row.ok && row.hi > 0 && l == 0.f;
+  if (__builtin_amdgcn_ballot_w64(empty) == 0) return ref;
+  uint64_t seen = 0;
+  for (int i = from; i < to; i += step) {
+    const int group0 = blocks.at(i) * (KB / kGroup);
+    pages.seek(a.b, s, group0);
+    seen |= seen_keys(row, group0 * kGroup, a.sinks, pages.keys<KB / kGroup>(group0));
+  }
+  return empty && seen ? kOnlyInf : ref;
+}
+
 template <int DH>
 __device__ __forceinline__ void load_q(const AttnArgs& a, const Row& row, int hg, u32x4_t (&qf)[Geo<DH>::DS]) {
   const bf16_t* q = static_cast<const bf16_t*>(a.q) + row.q_at;
@@ -473,7 +499,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Row& row, con
       }
     return;
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
+  const float inv = inverse_sum(l, st.t);
   bf16_t* o = static_cast<bf16_t*>(a.out) + row.out_at;
 #pragma unroll
   for (int t = 0; t < Geo<DH>::DT; ++t)
@@ -636,6 +662,7 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
     softmax_step<G, 2>(st, sc, vf, vb, key0, row, a.sinks, here, a.scale_log2, !whole);
   }
   const float l = st.l + __shfl_xor(st.l, 32, 64);
+  st.t = mark_seen<KB>(a, tile.s, blocks, from, to, 1, row, l, pages, st.t);
   store_row<DH>(a, row, st, l, hg, part);
 }
 
@@ -718,6 +745,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   // Join the waves' rows in pairs: the upper half of them leaves reference, sum
   // and output in LDS, the lower half takes them in.
   float l = st.l + __shfl_xor(st.l, 32, 64);
+  st.t = mark_seen<KB>(a, tile.s, blocks, from + wave, to, kWaves, row, l, pages, st.t);
   float* ol = reinterpret_cast<float*>(lds);
   float* ml = ol + (kWaves / 2) * 32 * OROW;
 #pragma unroll
@@ -933,12 +961,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
       if (u == qt) {
         const float l = l_run[u] + __shfl_xor(l_run[u], 16, 64);
         const float l4 = l + __shfl_xor(l, 32, 64);
+        Row row;
+        row.ok = 16 * u + c < tile.n;
+        row.hi = key_hi[u];
+        row.lo = key_lo[u];
+        const float m = mark_seen<KB>(a, tile.s, blocks, from + wave, to, kWaves, row, l4, pages, m_run[u]);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) part_o[wave][c * OROW + 16 * t + 4 * g + r] = acc[u][t][r];
         if (g == 0) {
-          part_m[wave][c] = m_run[u];
+          part_m[wave][c] = m;
           part_l[wave][c] = l4;
         }
       }
@@ -956,7 +989,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
     }
     const Row mine = make_row(a, tile, hk, 16 * qt + i);
     const bool last = a.parts == 1;
-    const float inv = last ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
+    const float inv = last ? inverse_sum(l, m) : 1.f;
     const long slot = mine.part * a.parts + part;
     float* out = last ? static_cast<float*>(a.out) + mine.out_at : a.ws_o + slot * DH;
     if (!last && (threadIdx.x & 15) == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * slot) = make_float2(m, l);
@@ -1032,7 +1065,7 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int r
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float inv = inverse_sum(l, m);
     T* out = static_cast<T*>(a.out) + row.out_at + d;
     if constexpr (sizeof(T) == 2)
       *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack2bf(x[0] * inv, x[1] * inv), pack2bf(x[2] * inv, x[3] * inv)};

@@ -105,3 +105,31 @@ def test_small_differences_of_large_scores(form, sign, q, k, unit):
     c = _case(form, 64, "bf16")
     _scores(c, [sign * q, unit], np.stack([np.full(TOKENS, float(k)), j], 1))
     _check(c, unit * j / 8, weights=2.0 ** -8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_scores_of_minus_infinity(dtype, form):
+    """Keys of -infinity have no weight; rows whose keys all are, and those alone,
+    are 0 / 0; rows that see no token stay zeros."""
+    c = _case(form, 64, dtype)
+    inf = np.full((TOKENS, 1), -np.inf)
+    _scores(c, [1.0], inf)
+    assert torch.isnan(c.run(False)).all() and torch.isnan(c.run(True, 40, 3)).all()
+    for at in ([0], [33], [600], [5, 333, 600]):
+        k = inf.copy()
+        k[at] = 2.0
+        _scores(c, [1.0], k)
+        _check(c, k[:, 0])
+    # causal, with a window: rows before token 400 and from 440 on see keys of
+    # -infinity alone
+    k = inf.copy()
+    k[400:410] = 1.0
+    _scores(c, [1.0], k)
+    out = c.run(True, 31, 0)
+    for s, n in enumerate(c.kv):
+        rows = slice(c.q_start[s], c.q_start[s + 1])
+        p = torch.arange(n - c.rows[s], n, device=DEV)
+        assert torch.equal(~torch.isnan(out[rows]).any(1), (p >= 400) & (p < 440))
+    c.table[:] = -1
+    assert torch.all(c.run(False) == 0)
