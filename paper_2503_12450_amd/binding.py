@@ -378,6 +378,13 @@ def _stream_here(device, stream) -> int:
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _int32(names: str, *sizes: int) -> None:
+    """Refuses what ctypes would cut to 32 bits without a word.  (The calls ask
+    only where any bit past 31 is set, which takes a fifth of the time.)"""
+    if max(sizes) >= 2 ** 31 or min(sizes) < -2 ** 31:
+        _refuse(f"{names} = {sizes}: more than 32 bits")
+
+
 def _storage_code(dtype) -> int:
     torch = _torch()
     if dtype is torch.bfloat16:
@@ -414,6 +421,7 @@ class Rotary:
             _refuse(f"unknown layout {layout!r}")
         _dense("freq", freq, torch.float64, (None,), freq.device)
         _dense("axis", axis, torch.int32, (freq.shape[0],), freq.device)
+        _int32("pairs, n_axes", freq.shape[0], n_axes)
         self.freq, self.axis, self.n_axes = freq, axis, n_axes
         self.device = freq.device
         self.c = MarRotaryC(freq.data_ptr(), axis.data_ptr(), freq.shape[0], n_axes, LAYOUTS[layout])
@@ -443,12 +451,15 @@ class PagedBatch:
         _dense("q_start", q_start, torch.int32, (table.shape[0] + 1,), dev)
         _dense("kv_len", kv_len, torch.int32, (table.shape[0],), dev)
         n_pages, heads, page, d_head = pages.k.shape
+        if max_kv is None:
+            max_kv = table.shape[1] * page
+        _int32("pages' shape, table's shape, max_kv", *pages.k.shape, *table.shape, max_kv)
         self.pages, self.table, self.q_start, self.kv_len = pages, table, q_start, kv_len
         self.dtype, self.device, self.d_head, self.heads = pages.k.dtype, dev, d_head, heads
         self.code = _storage_code(pages.k.dtype)
         self.c = MarPagedBatchC(pages.k.data_ptr(), pages.v.data_ptr(), table.data_ptr(), q_start.data_ptr(),
                                 kv_len.data_ptr(), n_pages, heads, page, d_head, table.shape[0], table.shape[1],
-                                table.shape[1] * page if max_kv is None else max_kv)
+                                max_kv)
         self.ref = ctypes.byref(self.c)
 
 
@@ -461,6 +472,8 @@ def k_rotary(rotary: Rotary, x, pos, out, d_head: int, stream=None) -> None:
     if heads_out != heads:
         _refuse("out and x differ in width")
     _dense("pos", pos, _torch().int32, (m, rotary.n_axes), dev)
+    if (m | heads | d_head) >> 31:
+        _int32("rows, heads, d_head", m, heads, d_head)
     _check(load().mar_k_rotary(_storage_code(dtype), rotary.ref, x.data_ptr(), ldx, pos.data_ptr(), m, heads, d_head,
                                out.data_ptr(), ldo, _stream_here(dev, stream)))
 
@@ -489,6 +502,8 @@ def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[
             _refuse("rotary needs pos, and its tables on the batch's GPU")
         _dense("pos", pos, _torch().int32, (m, rotary.n_axes), dev)
         rot, pos_ptr = rotary.ref, pos.data_ptr()
+    if (m | heads) >> 31:
+        _int32("rows, heads", m, heads)
     _check(load().mar_k_paged_store(batch.code, batch.ref, rot, pos_ptr, m, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                     heads, q_ptr, ldq, out_ptr, ldo, _stream_here(dev, stream)))
 
@@ -496,6 +511,7 @@ def k_paged_store(batch: PagedBatch, k, v, q=None, q_out=None, rotary: Optional[
 def paged_attention_workspace_bytes(batch: PagedBatch, m: int, n_heads_q: int, window: int = 0,
                                     sinks: int = 0) -> int:
     """Bytes of workspace that k_paged_attention makes use of for m rows."""
+    _int32("m, n_heads_q, window, sinks", m, n_heads_q, window, sinks)
     lib = load()
     n = lib.mar_k_paged_attention_workspace_bytes(batch.code, batch.ref, m, n_heads_q, window, sinks)
     if n == 0 and lib.mar_last_error():
@@ -519,6 +535,8 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
             _refuse("workspace: need a contiguous tensor on the batch's GPU")
         ws_bytes = workspace.numel() * workspace.element_size()
         ws_ptr = workspace.data_ptr() if ws_bytes else None
+    if (m | heads | window | sinks) >> 31:
+        _int32("rows, heads, window, sinks", m, heads, window, sinks)
     _check(load().mar_k_paged_attention(batch.code, batch.ref, m, heads, q.data_ptr(), ldq, 1 if causal else 0, window,
                                         sinks, ws_ptr, ws_bytes, out.data_ptr(), ldo, _stream_here(dev, stream)))
 

@@ -232,3 +232,29 @@ def test_binding_refuses_what_the_library_cannot_see():
     for call in bad:
         with pytest.raises(B.MarError):
             call()
+
+
+def test_binding_refuses_what_32_bits_do_not_hold():
+    """ctypes keeps the lower 32 bits of an int: a window of 2^32 + 5 would be one
+    of 5."""
+    pages = B.MarPages(torch.zeros(4, 2, 16, 32), torch.zeros(4, 2, 16, 32))
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)
+    table = torch.zeros((2, 2), dtype=torch.int32)
+    batch = B.PagedBatch(pages, table, i32(0, 1, 2), i32(3, 4))
+    rows, far = torch.zeros(2, 64), 2 ** 32
+    one = torch.zeros(1, 64).expand(far + 2, 64)   # rows without memory of their own
+    bad = [
+        lambda: B.PagedBatch(pages, table, i32(0, 1, 2), i32(3, 4), max_kv=far + 5),
+        lambda: B.Rotary(*B.rotary_sections((8, 8), device="cpu"), far + 2),
+        lambda: B.paged_attention_workspace_bytes(batch, far + 2, 2),
+        lambda: B.paged_attention_workspace_bytes(batch, 2, far + 2),
+        lambda: B.paged_attention_workspace_bytes(batch, 2, 2, window=far + 5),
+        lambda: B.paged_attention_workspace_bytes(batch, 2, 2, window=5, sinks=-far),
+        lambda: B.k_paged_attention(batch, rows, rows.clone(), window=far + 5),
+        lambda: B.k_paged_attention(batch, rows, rows.clone(), window=5, sinks=far),
+        lambda: B.k_paged_attention(batch, one, one),
+        lambda: B.k_paged_store(batch, one, one),
+    ]
+    for call in bad:
+        with pytest.raises(B.MarError, match="32 bits"):
+            call()
