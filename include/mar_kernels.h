@@ -131,9 +131,10 @@ mar_status mar_k_gemm_variant(int32_t variant);
  * What a kernel reads from the device it bounds itself: an entry of `table`
  * outside [0, n_pages) names no page (its keys are not visible, what is stored
  * there is dropped), tokens below 0 or at max_kv and above are not stored and
- * not visible, rows of no sequence (behind the last one, at m and above) are
- * left as they were.  q_start must ascend; otherwise which sequence a row
- * belongs to is undefined, but nothing outside the buffers is touched. */
+ * not visible, rows of no sequence (behind the last one) are left as they were,
+ * a sequence's rows at m and above are not there.  q_start must ascend;
+ * otherwise which sequence a row belongs to is undefined, but nothing outside the
+ * buffers is touched. */
 
 /* Which elements of a head make pair i of its n_pairs pairs: */
 typedef enum {

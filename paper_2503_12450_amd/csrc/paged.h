@@ -25,7 +25,8 @@ struct RotaryArgs {
 constexpr int kMaxTokens = 1 << 30;  // bound of every token number and of m * heads
 
 // A sequence's rows and tokens, bounded: rows [row0, row0 + n) of the m rows,
-// row i at token first + i, keys 0 .. len - 1 in the cache.  Whatever the
+// row i at token first + i (its last row, which may lie past m, at the last
+// token), keys 0 .. len - 1 in the cache.  Whatever the
 // device arrays hold, 0 <= row0, row0 + n <= m, 0 <= len <= max_kv and
 // |first + i| <= 2^30.
 struct SeqSpan {
@@ -34,9 +35,10 @@ struct SeqSpan {
 __device__ __forceinline__ SeqSpan seq_span(int start, int end, int kv_len, int max_kv, int m) {
   SeqSpan r;
   r.row0 = min(max(start, 0), m);
-  r.n = max(min(max(end, 0), m) - r.row0, 0);
+  end = min(max(end, 0), kMaxTokens);
+  r.n = max(min(end, m) - r.row0, 0);
   const int len = min(max(kv_len, 0), kMaxTokens);
-  r.first = len - r.n;
+  r.first = len - max(end - r.row0, 0);
   r.len = min(len, max_kv);
   return r;
 }
