@@ -23,7 +23,8 @@ namespace marcache {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxRows = 16;  // rows of a workgroup
+constexpr int kRowShift = 1;  // log2 of the rows of a workgroup, where there are enough
+constexpr int kMaxRows = 1 << kRowShift;
 constexpr int kMaxPairs = 64;
 
 struct RowArgs {
@@ -33,7 +34,7 @@ struct RowArgs {
   void* q_out;
   long ld_q, ld_k, ld_v, ld_q_out;
   int m, heads_q, d_head;
-  int row_shift;                 // log2 of the rows of a workgroup
+  int row_shift;                 // 0 or kRowShift
   int first;                     // row of workgroup 0
   Divisor by_units;              // d_head / 16 units of a head
 };
@@ -199,7 +200,7 @@ template <bool STORE>
 hipError_t launch_rows(int dtype, RowArgs& a, hipStream_t st) {
   const int heads = a.heads_q + (STORE ? 2 * a.b.n_heads : 0);
   if (a.m == 0 || heads == 0 || (STORE && a.b.n_seqs == 0)) return hipSuccess;
-  a.row_shift = a.m >= 4096 ? 1 : 0;
+  a.row_shift = a.m >= 4096 ? kRowShift : 0;
   a.by_units = make_divisor(a.d_head / 16);
   const int rows = 1 << a.row_shift;
   const long grid = (static_cast<long>(a.m) + rows - 1) / rows;
