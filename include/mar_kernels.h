@@ -162,7 +162,8 @@ typedef struct {
  * stores to.  k, v: 16-byte aligned.  page: a power of two, 16 .. 4096.
  * d_head: a multiple of 16, 16 .. 128.  max_kv bounds every kv_len
  * (1 <= max_kv <= max_pages * page <= 2^30): work is divided for that many
- * keys.  n_heads <= 4096, n_seqs <= 65536. */
+ * keys, so a bound far above the lengths leaves few workgroups to each of them.
+ * n_heads <= 4096, n_seqs <= 65536. */
 typedef struct {
   void *k, *v;            /* device [n_pages, n_heads, page, d_head] in dtype */
   const int32_t* table;   /* device [n_seqs, max_pages] */
@@ -194,8 +195,11 @@ mar_status mar_k_paged_store(int32_t dtype, const mar_paged_batch* batch, const 
 /* Attention of every row of the batch over its sequence's tokens in the cache:
  * q, out [m, n_heads_q * d_head], n_heads_q a multiple of batch->n_heads (query
  * head h reads key/value head h / (n_heads_q / batch->n_heads)), scale
- * 1/sqrt(d_head), softmax statistics in fp32.  The row at token p sees token j
- * of its sequence if
+ * 1/sqrt(d_head), softmax statistics and sums in fp32.  In bf16 the weights, up to
+ * 2^13 before they are divided by their sum, are rounded to bf16 for the product
+ * with the values, and the rounded ones are summed.  Finite values stay finite as
+ * long as |v| * (kv_len + 32) < 2^118.  The row at token p sees token j of its
+ * sequence if
  *   j < kv_len,  (not causal, or j <= p),
  *   (window == 0, or j > p - window, or j < sinks):
  * with a window the last `window` tokens up to its own, and the first `sinks`

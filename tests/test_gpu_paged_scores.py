@@ -133,3 +133,19 @@ def test_scores_of_minus_infinity(dtype, form):
         assert torch.equal(~torch.isnan(out[rows]).any(1), (p >= 400) & (p < 440))
     c.table[:] = -1
     assert torch.all(c.run(False) == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_values_up_to_the_bound(dtype, form):
+    """Equal values of the largest size that the header names, 2^118 / (kv_len +
+    32), under weights that grow by 2^7.7 behind the first blocks: they are their
+    own mean."""
+    c = _case(form, 64, dtype)
+    k = np.where(np.arange(TOKENS) < 100, 0.0, 43.0)[:, None]
+    _scores(c, [1.0], k)
+    size = 2.0 ** np.floor(np.log2(2.0 ** 118 / (max(c.kv) + 32)))
+    c.v.copy_(torch.where(torch.isnan(c.v), c.v, size))
+    _check(c, k[:, 0] / 8)
+    c.v.neg_()
+    _check(c, k[:, 0] / 8)
