@@ -565,8 +565,9 @@ __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_A
 // Bound by the vector ALU's part of the softmax (a quarter-rate exp2 per score)
 // and by LDS and memory latency that three waves a SIMD (two above d_head 64)
 // hide in part: 4 chunks of about 1000 rows on 15000 keys, 16 heads of 128 on 4,
-// take 540 us (890 TFLOP/s, matrix units 38 % busy); 31605 rows with a window of
-// 1024, 16 heads of 64: 198 us (690 TFLOP/s, vector ALUs 72 % busy).  Tiles of 256
+// take 525 us (913 TFLOP/s, matrix units 37 % busy; 105 scalars
+// spilled to vector registers); 31605 rows with a window of 1024, 16 heads of 64:
+// 199 us (684 TFLOP/s, vector ALUs 72 % busy).  Tiles of 256
 // rows (eight waves, or 64 rows to a wave) halve the copies or the LDS reads, but
 // leave fewer waves to hide them and are slower.
 template <int DH, int RING>
