@@ -184,9 +184,13 @@ def _stream(stream=None) -> int:
     if stream is not None:
         return stream.cuda_stream
     torch = _torch()
+    device = torch.cuda.current_device()
     # the current stream's handle without a Stream object around it (0.3 us
     # instead of 2.8, of a call that takes 4 to launch a small kernel)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    try:
+        return torch._C._cuda_getCurrentRawStream(device)
+    except AttributeError:  # not a public name
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def workspace_bytes(dims) -> int:
@@ -375,7 +379,12 @@ def _stream_here(device, stream) -> int:
     torch = _torch()
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         _refuse(f"the tensors are on {device}: need the current GPU")
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+    if stream is not None:
+        return stream.cuda_stream
+    try:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    except AttributeError:
+        return _stream()
 
 
 def _int32(names: str, *sizes: int) -> None:

@@ -258,3 +258,16 @@ def test_binding_refuses_what_32_bits_do_not_hold():
     for call in bad:
         with pytest.raises(B.MarError, match="32 bits"):
             call()
+
+
+def test_the_current_stream_without_the_private_call(monkeypatch):
+    """Where torch has no raw handle to give, its Stream object's is taken."""
+    class Stream:
+        cuda_stream = 1234
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream())
+    assert B._stream() == 1234 and B._stream_here(torch.device("cuda", 0), None) == 1234
+    other = Stream()
+    other.cuda_stream = 99
+    assert B._stream(other) == 99 and B._stream_here(torch.device("cuda", 0), other) == 99
