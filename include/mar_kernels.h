@@ -225,6 +225,125 @@ mar_status mar_k_paged_attention(int32_t dtype, const mar_paged_batch* batch, in
 size_t mar_k_paged_attention_workspace_bytes(int32_t dtype, const mar_paged_batch* batch, int32_t m,
                                              int32_t n_heads_q, int32_t window, int32_t sinks);
 
+/* ---------------------------------------------------------------------------
+ * Drafted tokens: several guesses at the tokens to come are computed in one
+ * step, as the nodes of a tree that grows on a sequence's past, and those that
+ * the target model itself would have drawn are kept.
+ *
+ * A sequence's rows are its tree's nodes: parent[row] names the node that row
+ * i hangs on, by its number in the sequence (0 <= parent < i; anything else: it
+ * hangs on the past).  A chain is parent = i - 1.  Their keys and values are
+ * stored as any new tokens' (mar_k_paged_store, row i as token kv_len - n + i),
+ * rotated to the position of their depth.  A step, each of its calls reading what
+ * the one before left on the device:
+ *   mar_k_paged_store, mar_k_paged_tree_attention   in every layer
+ *   mar_k_probabilities                             of the rows' logits
+ *   mar_k_draft_verify                              which nodes are kept
+ *   mar_k_paged_keep                                their rows moved together, in
+ *                                                   every layer's pages
+ *   mar_k_paged_fork                                room for the next step */
+
+/* Attention of the nodes of trees over the cache: as mar_k_paged_attention, but
+ * for what a row sees.  With first = kv_len - n the token of node 0 and depth the
+ * number of a node's ancestors, the node lies at position first + depth and sees
+ *   token j < first  if window == 0, or j > first + depth - window, or j < sinks,
+ *   itself, and an ancestor whose position passes the same test.
+ * A sequence's nodes from the 256th on are left as they were in out.  Workspace,
+ * strides, roundings, empty rows and values that are not finite as there. */
+mar_status mar_k_paged_tree_attention(int32_t dtype, const mar_paged_batch* batch, int32_t m, int32_t n_heads_q,
+                                      const void* q, int64_t ld_q, const int32_t* parent, int32_t window,
+                                      int32_t sinks, void* workspace, size_t workspace_bytes, void* out,
+                                      int64_t ld_out, void* stream);
+
+/* Bytes of workspace that mar_k_paged_tree_attention makes use of (0 if none, or
+ * if an argument is refused; mar_last_error() then says why). */
+size_t mar_k_paged_tree_attention_workspace_bytes(int32_t dtype, const mar_paged_batch* batch, int32_t m,
+                                                  int32_t n_heads_q, int32_t window, int32_t sinks);
+
+/* out[m, vocab] (fp32) = probabilities of the rows of logits (in dtype):
+ *   exp((x - max) / T) / sum of the row's, in fp32,
+ * T = temperature[row] (device, fp32; NULL: 1 everywhere).  Of a temperature that
+ * is not above 2^-100 (0, negative, NaN) the row's first largest value gets 1 and
+ * the rest 0 (NaN is never the largest; a row without a value above -infinity
+ * is zeros).  Otherwise -infinity has probability 0, and a row with a NaN or
+ * +infinity, or without a finite value, is NaN.  Any row strides from vocab on
+ * (< 2^31, elements); logits and out aligned to their elements; out may be logits
+ * itself in fp32 (same pointer and stride), else they must not overlap.  m <
+ * 2^30, 1 <= vocab <= 2^20. */
+mar_status mar_k_probabilities(int32_t dtype, const void* logits, int64_t ld, const float* temperature, int32_t m,
+                               int32_t vocab, float* out, int64_t ld_out, void* stream);
+
+/* Which nodes of each sequence's tree (rows q_start[s] .. q_start[s + 1] - 1) are
+ * kept, and the token after them.  Node 0 is the known last token of the sequence
+ * and always kept; tokens[row] is the token of every other one; row `row` of p
+ * [m, vocab] (in dtype) holds the target's probabilities of the token after it.
+ * From cur = 0, weights w = p[0], W = 1 the nodes are looked at in ascending order,
+ * each with parent cur:
+ *   draft NULL (a token is proposed as it is): kept if random[row] W < w[token]; if
+ *     not, W -= w[token] and w[token] = 0;
+ *   draft given (the children of a node were drawn from row cur of draft [m,
+ *     vocab], each on its own): kept if random[row] draft[token] W < w[token]; if
+ *     not, w = max(w / W - draft, 0) and W its sum (unless that is 0: then both
+ *     stay);
+ *   kept: cur = the node, w = p[cur], W = 1.
+ * next[s] is the first token x with w[0] + .. + w[x] > random[node 0's row] * (sum
+ * of w): the last one with a weight if there is none (a random number of 1 or
+ * more, or NaN), -1 if none has a weight.  With random numbers that are uniform
+ * on [0, 1) the kept tokens and the next one are distributed as if drawn from
+ * p one after the other.  random NULL (draft too): greedy, a node is kept if
+ * its token is the first largest of p[cur], which is also next (p may be
+ * logits; NaN is never the largest; -1 if nothing is above -infinity).  A
+ * sequence's nodes from the 256th on are never kept.
+ *   path[q_start[s] + k] = the k-th kept node, from 0 on, -1 behind the last
+ *   kept[s] = their number (0, with next -1, if the sequence has no rows)
+ * Entries of path of no sequence stay as they were.  Values of p and draft that are
+ * no probabilities (negative, infinite, NaN) count as 0, tokens outside [0, vocab)
+ * are never kept.  Products and sums in fp64, the sums in a fixed order.  Row
+ * strides, alignment and vocab as in mar_k_probabilities; m < 2^30, n_seqs <=
+ * 65536.  workspace: device, 16-byte aligned, of at least
+ * mar_k_draft_verify_workspace_bytes; calls that may overlap need one each. */
+mar_status mar_k_draft_verify(int32_t dtype, int32_t n_seqs, const int32_t* q_start, int32_t m, int32_t vocab,
+                              const void* p, int64_t ld_p, const void* draft, int64_t ld_draft, const int32_t* parent,
+                              const int32_t* tokens, const float* random, int32_t* path, int32_t* kept, int32_t* next,
+                              void* workspace, size_t workspace_bytes, void* stream);
+/* (0 also if an argument is refused; mar_last_error() then says why.) */
+size_t mar_k_draft_verify_workspace_bytes(int32_t m, int32_t n_seqs, int32_t vocab);
+
+/* The kept nodes' keys and values moved together: with first = kv_len - n as
+ * above, token first + path[k] goes to the place of token first + k for every k <
+ * kept[s] (path [m] ascending, as mar_k_draft_verify leaves it), and kv_len_out[s]
+ * = first + kept[s] (kv_len[s] of a sequence without rows).  Nodes that path names
+ * out of order or outside the sequence, and tokens without a place, are not moved.
+ * kv_len_out must not be kv_len.  Pages that other sequences read must not hold
+ * new tokens, as for the store. */
+mar_status mar_k_paged_keep(int32_t dtype, const mar_paged_batch* batch, int32_t m, const int32_t* path,
+                            const int32_t* kept, int32_t* kv_len_out, void* stream);
+
+/* A table for the next step, in place of the batch's: row i of table_out [n_new,
+ * max_pages] continues sequence source[i] (outside [0, n_seqs): a new one, empty)
+ * with its first keep[i] tokens (NULL: all kv_len of them; bounded by that) and
+ * has room for add[i] more (NULL: none; bounded by max_pages * page): kv_len_out[i]
+ * = keep + add.  Any number of rows may continue the same sequence, or none (its
+ * pages are free then, as are those behind a sequence's keep).
+ *   Pages that stay are shared.  The last one kept, if part of it is free and the
+ * row will write there (add > 0), is copied unless nobody else in the new table
+ * names it, or all who do will write to it and the row is the lowest of them: the
+ * copy holds its kept tokens.
+ *   Fresh pages, for copies and new tokens, are those that no sequence of the batch
+ * holds within its kv_len, the lowest first, in the order of the new rows and
+ * their slots; table entries behind the last one needed are -1.  missing[0] is the
+ * number of pages that there were too few of: the last rows' entries are then -1,
+ * and a copy that got none is lost with its kept tokens (they are not visible).
+ * Pages taken from the old sequences by this call are free from the next one on.
+ * The tables and kv_len_out must not overlap.  q_start is not read.  n_new <= 65536.
+ * workspace: device, 16-byte aligned, of at least
+ * mar_k_paged_fork_workspace_bytes; calls that may overlap need one each. */
+mar_status mar_k_paged_fork(int32_t dtype, const mar_paged_batch* batch, int32_t n_new, const int32_t* source,
+                            const int32_t* keep, const int32_t* add, int32_t* table_out, int32_t* kv_len_out,
+                            int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);
+/* (0 if an argument is refused; mar_last_error() then says why.) */
+size_t mar_k_paged_fork_workspace_bytes(const mar_paged_batch* batch, int32_t n_new);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,6 +34,9 @@ EXPORTED = (
     "mar_k_attention", "mar_k_scores", "mar_k_select", "mar_k_select_most_similar",
     "mar_k_gemm_variant",
     "mar_k_rotary", "mar_k_paged_store", "mar_k_paged_attention", "mar_k_paged_attention_workspace_bytes",
+    "mar_k_paged_tree_attention", "mar_k_paged_tree_attention_workspace_bytes", "mar_k_probabilities",
+    "mar_k_draft_verify", "mar_k_draft_verify_workspace_bytes", "mar_k_paged_keep", "mar_k_paged_fork",
+    "mar_k_paged_fork_workspace_bytes",
     "mar_head_workspace_bytes", "mar_head_init", "mar_head_sample", "mar_head_destroy",
     "mar_head_sample_noalloc",
 )
@@ -120,6 +123,18 @@ _SIGNATURES = {
     "mar_k_paged_attention": (_i32, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _i32, _vp, _i64, _i32, _i32, _i32,
                                      _vp, _sz, _vp, _i64, _vp]),
     "mar_k_paged_attention_workspace_bytes": (_sz, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _i32, _i32, _i32]),
+    "mar_k_paged_tree_attention": (_i32, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _i32, _vp, _i64, _vp, _i32, _i32,
+                                          _vp, _sz, _vp, _i64, _vp]),
+    "mar_k_paged_tree_attention_workspace_bytes": (_sz, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _i32, _i32,
+                                                         _i32]),
+    "mar_k_probabilities": (_i32, [_i32, _vp, _i64, _vp, _i32, _i32, _vp, _i64, _vp]),
+    "mar_k_draft_verify": (_i32, [_i32, _i32, _vp, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
+                                  _vp, _sz, _vp]),
+    "mar_k_draft_verify_workspace_bytes": (_sz, [_i32, _i32, _i32]),
+    "mar_k_paged_keep": (_i32, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _vp, _vp, _vp, _vp]),
+    "mar_k_paged_fork": (_i32, [_i32, ctypes.POINTER(MarPagedBatchC), _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                _vp]),
+    "mar_k_paged_fork_workspace_bytes": (_sz, [ctypes.POINTER(MarPagedBatchC), _i32]),
     "mar_head_workspace_bytes": (_sz, [ctypes.POINTER(MarHeadDimsC)]),
     "mar_head_init": (_i32, [ctypes.POINTER(MarHeadDimsC), ctypes.POINTER(MarHeadWeightsC), _vp, _sz, _vp,
                              ctypes.POINTER(_vp)]),
@@ -549,6 +564,167 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
         _int32("rows, heads, window, sinks", m, heads, window, sinks)
     _check(load().mar_k_paged_attention(batch.code, batch.ref, m, heads, q.data_ptr(), ldq, 1 if causal else 0, window,
                                         sinks, ws_ptr, ws_bytes, out.data_ptr(), ldo, _stream_here(dev, stream)))
+
+
+# --------------------------------------------------------------------------
+# drafted tokens
+# --------------------------------------------------------------------------
+
+def _workspace(workspace, device):
+    """(pointer, bytes) of a workspace tensor of any type, or of None."""
+    if workspace is None:
+        return None, 0
+    if workspace.device != device or not workspace.is_contiguous():
+        _refuse(f"workspace: need a contiguous tensor on {device}")
+    n = workspace.numel() * workspace.element_size()
+    return workspace.data_ptr() if n else None, n
+
+
+def _vocab_rows(name: str, t, dtype, shape, device) -> int:
+    """Row stride of t [m, vocab] with dense columns on `device` (a single row's
+    counts as dense)."""
+    have, stride = t.shape, t.stride()
+    if t.dtype is dtype and have == shape and (stride[1] == 1 or have[1] == 1) and t.device == device:
+        return stride[0] if have[0] > 1 else have[1]
+    _refuse(f"{name}: need {tuple(shape)} with dense columns, {dtype} on {device}, got {tuple(have)} with strides "
+            f"{stride}, {t.dtype} on {t.device}")
+
+
+def paged_tree_attention_workspace_bytes(batch: PagedBatch, m: int, n_heads_q: int, window: int = 0,
+                                         sinks: int = 0) -> int:
+    """Bytes of workspace that k_paged_tree_attention makes use of for m rows."""
+    _int32("m, n_heads_q, window, sinks", m, n_heads_q, window, sinks)
+    lib = load()
+    n = lib.mar_k_paged_tree_attention_workspace_bytes(batch.code, batch.ref, m, n_heads_q, window, sinks)
+    if n == 0 and lib.mar_last_error():
+        raise MarError(MAR_E_ARG, lib.mar_last_error().decode())
+    return n
+
+
+def k_paged_tree_attention(batch: PagedBatch, q, parent, out, window: int = 0, sinks: int = 0, workspace=None,
+                           stream=None) -> None:
+    """Attention of the rows q [m, heads * d_head], the nodes of their sequences'
+    trees (parent [m] int32: number of a row's parent in its sequence, or -1), over
+    the past, themselves and their ancestors."""
+    m, dev, dh, dtype = q.shape[0], batch.device, batch.d_head, batch.dtype
+    heads, ldq = _rows("q", q, dtype, m, dh, dev)
+    heads_out, ldo = _rows("out", out, dtype, m, dh, dev)
+    if heads_out != heads:
+        _refuse("out and q differ in width")
+    _dense("parent", parent, _torch().int32, (m,), dev)
+    ws_ptr, ws_bytes = _workspace(workspace, dev)
+    if (m | heads | window | sinks) >> 31:
+        _int32("rows, heads, window, sinks", m, heads, window, sinks)
+    _check(load().mar_k_paged_tree_attention(batch.code, batch.ref, m, heads, q.data_ptr(), ldq, parent.data_ptr(),
+                                             window, sinks, ws_ptr, ws_bytes, out.data_ptr(), ldo,
+                                             _stream_here(dev, stream)))
+
+
+def k_probabilities(logits, out, temperature=None, stream=None) -> None:
+    """out [m, vocab] fp32 = probabilities of the logits' rows at temperature [m]
+    fp32 (None: 1; 0: one at the first largest logit)."""
+    torch = _torch()
+    dev, dtype, shape = logits.device, logits.dtype, logits.shape
+    if len(shape) != 2:
+        _refuse(f"logits: need [m, vocab], got {tuple(shape)}")
+    ld = _vocab_rows("logits", logits, dtype, shape, dev)
+    ldo = _vocab_rows("out", out, torch.float32, shape, dev)
+    m, vocab = shape
+    if temperature is not None:
+        _dense("temperature", temperature, torch.float32, (m,), dev)
+    if (m | vocab) >> 31:
+        _int32("logits' shape", m, vocab)
+    _check(load().mar_k_probabilities(_storage_code(dtype), logits.data_ptr(), ld, _ptr(temperature), m, vocab,
+                                      out.data_ptr(), ldo, _stream_here(dev, stream)))
+
+
+def draft_verify_workspace_bytes(m: int, n_seqs: int, vocab: int) -> int:
+    """Bytes of workspace that k_draft_verify needs."""
+    _int32("m, n_seqs, vocab", m, n_seqs, vocab)
+    lib = load()
+    n = lib.mar_k_draft_verify_workspace_bytes(m, n_seqs, vocab)
+    if n == 0 and lib.mar_last_error():
+        raise MarError(MAR_E_ARG, lib.mar_last_error().decode())
+    return n
+
+
+def k_draft_verify(q_start, p, parent, tokens, path, kept, next_token, random=None, draft=None, workspace=None,
+                   stream=None) -> None:
+    """Which nodes of the trees [q_start[s], q_start[s + 1]) the probabilities p [m,
+    vocab] keep: path [m], kept [n_seqs], and next_token [n_seqs] after them.
+    random [m] fp32: a number in [0, 1) per node, node 0's for the next token
+    (None: greedy); draft [m, vocab]: probabilities that a node's children were
+    drawn from (None: they are proposed as they are)."""
+    torch = _torch()
+    dev, dtype, shape = p.device, p.dtype, p.shape
+    if len(shape) != 2 or len(q_start.shape) != 1 or q_start.shape[0] < 1:
+        _refuse("need p [m, vocab] and q_start [n_seqs + 1]")
+    ldp = _vocab_rows("p", p, dtype, shape, dev)
+    ldd = _vocab_rows("draft", draft, dtype, shape, dev) if draft is not None else 0
+    m, vocab = shape
+    n_seqs, i32 = q_start.shape[0] - 1, torch.int32
+    _dense("q_start", q_start, i32, (n_seqs + 1,), dev)
+    _dense("parent", parent, i32, (m,), dev)
+    _dense("tokens", tokens, i32, (m,), dev)
+    _dense("path", path, i32, (m,), dev)
+    _dense("kept", kept, i32, (n_seqs,), dev)
+    _dense("next_token", next_token, i32, (n_seqs,), dev)
+    if random is not None:
+        _dense("random", random, torch.float32, (m,), dev)
+    ws_ptr, ws_bytes = _workspace(workspace, dev)
+    if (m | vocab | n_seqs) >> 31:
+        _int32("m, vocab, n_seqs", m, vocab, n_seqs)
+    _check(load().mar_k_draft_verify(_storage_code(dtype), n_seqs, q_start.data_ptr(), m, vocab, p.data_ptr(), ldp,
+                                     _ptr(draft), ldd, parent.data_ptr(), tokens.data_ptr(), _ptr(random),
+                                     path.data_ptr(), kept.data_ptr(), next_token.data_ptr(), ws_ptr, ws_bytes,
+                                     _stream_here(dev, stream)))
+
+
+def k_paged_keep(batch: PagedBatch, path, kept, kv_len_out, stream=None) -> None:
+    """The kept nodes' keys and values (path [m], kept [seqs] as k_draft_verify
+    leaves them) moved together in the batch's pages; kv_len_out [seqs]: the
+    lengths that remain."""
+    dev, i32, n = batch.device, _torch().int32, batch.kv_len.shape[0]
+    m = path.shape[0] if len(path.shape) == 1 else -1
+    _dense("path", path, i32, (None,), dev)
+    _dense("kept", kept, i32, (n,), dev)
+    _dense("kv_len_out", kv_len_out, i32, (n,), dev)
+    if m >> 31:
+        _int32("rows", m)
+    _check(load().mar_k_paged_keep(batch.code, batch.ref, m, path.data_ptr(), kept.data_ptr(), kv_len_out.data_ptr(),
+                                   _stream_here(dev, stream)))
+
+
+def paged_fork_workspace_bytes(batch: PagedBatch, n_new: int) -> int:
+    """Bytes of workspace that k_paged_fork needs for n_new rows."""
+    _int32("n_new", n_new)
+    lib = load()
+    n = lib.mar_k_paged_fork_workspace_bytes(batch.ref, n_new)
+    if n == 0:
+        raise MarError(MAR_E_ARG, lib.mar_last_error().decode())
+    return n
+
+
+def k_paged_fork(batch: PagedBatch, source, table_out, kv_len_out, missing, keep=None, add=None, workspace=None,
+                 stream=None) -> None:
+    """A new table: row i continues sequence source[i] with its first keep[i]
+    tokens (None: all) and room for add[i] more (None: none).  table_out [n,
+    max_pages], kv_len_out [n], missing [1]; source, keep, add [n]; all int32."""
+    dev, i32 = batch.device, _torch().int32
+    _dense("source", source, i32, (None,), dev)
+    n = source.shape[0]
+    _dense("table_out", table_out, i32, (n, batch.table.shape[1]), dev)
+    _dense("kv_len_out", kv_len_out, i32, (n,), dev)
+    _dense("missing", missing, i32, (1,), dev)
+    for name, t in (("keep", keep), ("add", add)):
+        if t is not None:
+            _dense(name, t, i32, (n,), dev)
+    ws_ptr, ws_bytes = _workspace(workspace, dev)
+    if n >> 31:
+        _int32("rows", n)
+    _check(load().mar_k_paged_fork(batch.code, batch.ref, n, source.data_ptr(), _ptr(keep), _ptr(add),
+                                   table_out.data_ptr(), kv_len_out.data_ptr(), missing.data_ptr(), ws_ptr, ws_bytes,
+                                   _stream_here(dev, stream)))
 
 
 # --------------------------------------------------------------------------

@@ -53,4 +53,18 @@ hipError_t launch_paged_attention(int dtype, const PagedBatch& b, int m, int hea
                                   long ld_out, hipStream_t st);
 size_t paged_attention_workspace(int dtype, const PagedBatch& b, int m, int heads_q, int window, int sinks);
 
+// Trees of drafted tokens: a sequence's first kMaxTree new rows.
+constexpr int kMaxTree = 256;
+hipError_t launch_tree_attention(int dtype, const PagedBatch& b, int m, int heads_q, const void* q, long ld_q,
+                                 const int32_t* parent, int window, int sinks, void* ws, size_t ws_bytes, void* out,
+                                 long ld_out, hipStream_t st);
+size_t tree_attention_workspace(int dtype, const PagedBatch& b, int m, int heads_q, int window, int sinks);
+
+hipError_t launch_paged_keep(int dtype, const PagedBatch& b, int m, const int32_t* path, const int32_t* kept,
+                             int32_t* kv_out, hipStream_t st);
+hipError_t launch_paged_fork(int dtype, const PagedBatch& b, int n_new, const int32_t* source, const int32_t* keep,
+                             const int32_t* add, int32_t* table_out, int32_t* kv_out, int32_t* missing, void* ws,
+                             hipStream_t st);
+size_t paged_fork_workspace(const PagedBatch& b, int n_new);
+
 }  // namespace marcache

@@ -1,10 +1,12 @@
-// C entry points of the rotary positions, the paged cache and its attention:
-// every argument is checked here, on the host, before anything is enqueued.
+// C entry points of the rotary positions, the paged cache, its attention and what
+// decides about drafted tokens: every argument is checked here, on the host,
+// before anything is enqueued.
 #include <hip/hip_runtime.h>
 
 #include <cstdarg>
 
 #include "../../include/mar_kernels.h"
+#include "draft.h"
 #include "paged.h"
 
 using namespace marcache;
@@ -92,6 +94,40 @@ mar_status take_attention(int32_t dtype, const mar_paged_batch* batch, int32_t m
   return MAR_OK;
 }
 
+// Rows of `vocab` elements of es bytes at p, row stride ld
+mar_status check_vocab_rows(const char* name, const void* p, int64_t ld, int32_t m, int32_t vocab, unsigned es) {
+  if (ld < vocab || ld >= (int64_t{1} << 31))
+    return fail(MAR_E_SHAPE, "%s: row stride %lld must cover %d tokens", name, static_cast<long long>(ld), vocab);
+  if (m > 0 && !p) return fail(MAR_E_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % es) return fail(MAR_E_ARG, "%s must be aligned to its elements", name);
+  return MAR_OK;
+}
+
+mar_status check_vocab(int32_t m, int32_t vocab) {
+  if (m < 0 || m >= kMaxTokens) return fail(MAR_E_SHAPE, "need 0 <= m < 2^30");
+  if (vocab < 1 || vocab > kMaxVocab) return fail(MAR_E_SHAPE, "vocab %d outside [1, %d]", vocab, kMaxVocab);
+  return MAR_OK;
+}
+
+mar_status check_verify(int32_t m, int32_t n_seqs, int32_t vocab) {
+  if (n_seqs < 0 || n_seqs > 65536) return fail(MAR_E_SHAPE, "n_seqs %d outside [0, 65536]", n_seqs);
+  return check_vocab(m, vocab);
+}
+
+mar_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (have < need) return fail(MAR_E_WORKSPACE, "workspace of %zu bytes, need %zu", have, need);
+  if (need && !ws) return fail(MAR_E_WORKSPACE, "workspace is NULL");
+  if (!aligned16(ws)) return fail(MAR_E_WORKSPACE, "workspace must be 16-byte aligned");
+  return MAR_OK;
+}
+
+mar_status take_fork(const mar_paged_batch* batch, int32_t n_new, PagedBatch* b) {
+  const mar_status s = take_batch(batch, b);
+  if (s != MAR_OK) return s;
+  if (n_new < 0 || n_new > 65536) return fail(MAR_E_SHAPE, "n_new %d outside [0, 65536]", n_new);
+  return MAR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -160,6 +196,113 @@ mar_status mar_k_paged_attention(int32_t dtype, const mar_paged_batch* batch, in
   return device_result(launch_paged_attention(dtype, b, m, n_heads_q, q, ld_q, causal != 0, window, sinks, workspace,
                                               workspace_bytes, out, ld_out, static_cast<hipStream_t>(stream)),
                        "paged attention");
+}
+
+size_t mar_k_paged_tree_attention_workspace_bytes(int32_t dtype, const mar_paged_batch* batch, int32_t m,
+                                                  int32_t n_heads_q, int32_t window, int32_t sinks) {
+  abi_clear_error();
+  PagedBatch b;
+  if (take_attention(dtype, batch, m, n_heads_q, window, sinks, &b) != MAR_OK) return 0;
+  return tree_attention_workspace(dtype, b, m, n_heads_q, window, sinks);
+}
+
+mar_status mar_k_paged_tree_attention(int32_t dtype, const mar_paged_batch* batch, int32_t m, int32_t n_heads_q,
+                                      const void* q, int64_t ld_q, const int32_t* parent, int32_t window,
+                                      int32_t sinks, void* workspace, size_t workspace_bytes, void* out,
+                                      int64_t ld_out, void* stream) {
+  abi_clear_error();
+  PagedBatch b;
+  mar_status s = take_attention(dtype, batch, m, n_heads_q, window, sinks, &b);
+  if (s == MAR_OK) s = check_rows("q", q, ld_q, m, n_heads_q, b.d_head);
+  if (s == MAR_OK) s = check_rows("out", out, ld_out, m, n_heads_q, b.d_head);
+  if (s == MAR_OK && m > 0 && !parent) s = fail(MAR_E_ARG, "parent is NULL");
+  if (s == MAR_OK && m > 0 && out == q) s = fail(MAR_E_ARG, "out must not be q");
+  if (s == MAR_OK && !workspace && workspace_bytes) s = fail(MAR_E_WORKSPACE, "workspace is NULL");
+  if (s == MAR_OK && !aligned16(workspace)) s = fail(MAR_E_WORKSPACE, "workspace must be 16-byte aligned");
+  if (s != MAR_OK) return s;
+  return device_result(launch_tree_attention(dtype, b, m, n_heads_q, q, ld_q, parent, window, sinks, workspace,
+                                             workspace_bytes, out, ld_out, static_cast<hipStream_t>(stream)),
+                       "tree attention");
+}
+
+mar_status mar_k_probabilities(int32_t dtype, const void* logits, int64_t ld, const float* temperature, int32_t m,
+                               int32_t vocab, float* out, int64_t ld_out, void* stream) {
+  abi_clear_error();
+  mar_status s = check_dtype(dtype);
+  if (s == MAR_OK) s = check_vocab(m, vocab);
+  if (s == MAR_OK) s = check_vocab_rows("logits", logits, ld, m, vocab, dtype == MAR_BF16 ? 2 : 4);
+  if (s == MAR_OK) s = check_vocab_rows("out", out, ld_out, m, vocab, 4);
+  if (s == MAR_OK && m > 0 && static_cast<const void*>(out) == logits && (dtype != MAR_F32 || ld != ld_out))
+    s = fail(MAR_E_ARG, "out may be logits only in fp32 with the same row stride");
+  if (s != MAR_OK) return s;
+  return device_result(launch_probabilities(dtype, logits, ld, temperature, m, vocab, out, ld_out,
+                                            static_cast<hipStream_t>(stream)),
+                       "probabilities");
+}
+
+size_t mar_k_draft_verify_workspace_bytes(int32_t m, int32_t n_seqs, int32_t vocab) {
+  abi_clear_error();
+  if (check_verify(m, n_seqs, vocab) != MAR_OK) return 0;
+  return verify_workspace(m, n_seqs, vocab);
+}
+
+mar_status mar_k_draft_verify(int32_t dtype, int32_t n_seqs, const int32_t* q_start, int32_t m, int32_t vocab,
+                              const void* p, int64_t ld_p, const void* draft, int64_t ld_draft, const int32_t* parent,
+                              const int32_t* tokens, const float* random, int32_t* path, int32_t* kept, int32_t* next,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  abi_clear_error();
+  const unsigned es = dtype == MAR_BF16 ? 2 : 4;
+  mar_status s = check_dtype(dtype);
+  if (s == MAR_OK) s = check_verify(m, n_seqs, vocab);
+  if (s == MAR_OK) s = check_vocab_rows("p", p, ld_p, m, vocab, es);
+  if (s == MAR_OK && draft) s = check_vocab_rows("draft", draft, ld_draft, m, vocab, es);
+  if (s == MAR_OK && draft && !random) s = fail(MAR_E_ARG, "draft needs random numbers");
+  if (s == MAR_OK && n_seqs > 0 && (!q_start || !kept || !next)) s = fail(MAR_E_ARG, "NULL pointer");
+  if (s == MAR_OK && m > 0 && (!parent || !tokens || !path)) s = fail(MAR_E_ARG, "NULL pointer");
+  if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, verify_workspace(m, n_seqs, vocab));
+  if (s != MAR_OK) return s;
+  const VerifyArgs a{p,    draft, q_start, parent, tokens,   random, path,   kept,
+                     next, workspace, ld_p, ld_draft, m, n_seqs, vocab};
+  return device_result(launch_verify(dtype, a, static_cast<hipStream_t>(stream)), "draft verify");
+}
+
+mar_status mar_k_paged_keep(int32_t dtype, const mar_paged_batch* batch, int32_t m, const int32_t* path,
+                            const int32_t* kept, int32_t* kv_len_out, void* stream) {
+  abi_clear_error();
+  PagedBatch b;
+  mar_status s = check_dtype(dtype);
+  if (s == MAR_OK) s = take_batch(batch, &b);
+  if (s == MAR_OK && (m < 0 || m >= kMaxTokens)) s = fail(MAR_E_SHAPE, "need 0 <= m < 2^30");
+  if (s == MAR_OK && ((m > 0 && !path) || (b.n_seqs > 0 && (!kept || !kv_len_out)))) s = fail(MAR_E_ARG, "NULL pointer");
+  if (s == MAR_OK && b.n_seqs > 0 && kv_len_out == b.kv_len) s = fail(MAR_E_ARG, "kv_len_out must not be kv_len");
+  if (s != MAR_OK) return s;
+  return device_result(launch_paged_keep(dtype, b, m, path, kept, kv_len_out, static_cast<hipStream_t>(stream)),
+                       "paged keep");
+}
+
+size_t mar_k_paged_fork_workspace_bytes(const mar_paged_batch* batch, int32_t n_new) {
+  abi_clear_error();
+  PagedBatch b;
+  if (take_fork(batch, n_new, &b) != MAR_OK) return 0;
+  return paged_fork_workspace(b, n_new);
+}
+
+mar_status mar_k_paged_fork(int32_t dtype, const mar_paged_batch* batch, int32_t n_new, const int32_t* source,
+                            const int32_t* keep, const int32_t* add, int32_t* table_out, int32_t* kv_len_out,
+                            int32_t* missing, void* workspace, size_t workspace_bytes, void* stream) {
+  abi_clear_error();
+  PagedBatch b;
+  mar_status s = check_dtype(dtype);
+  if (s == MAR_OK) s = take_fork(batch, n_new, &b);
+  if (s == MAR_OK && (!missing || (n_new > 0 && (!source || !table_out || !kv_len_out))))
+    s = fail(MAR_E_ARG, "NULL pointer");
+  if (s == MAR_OK && n_new > 0 && (table_out == b.table || kv_len_out == b.kv_len))
+    s = fail(MAR_E_ARG, "table_out and kv_len_out must not be the batch's");
+  if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, paged_fork_workspace(b, n_new));
+  if (s != MAR_OK) return s;
+  return device_result(launch_paged_fork(dtype, b, n_new, source, keep, add, table_out, kv_len_out, missing, workspace,
+                                         static_cast<hipStream_t>(stream)),
+                       "paged fork");
 }
 
 }  // extern "C"
