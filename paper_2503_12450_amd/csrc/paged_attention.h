@@ -37,6 +37,8 @@ constexpr float kRough = 4096.f;  // see softmax_step
 constexpr int kWaves = 4;
 constexpr int kGroup = 16;  // keys that always lie in one page
 constexpr int kTreeWords = kMaxTree / 64;
+constexpr int kXcds = 8;
+constexpr int kTileRun = 4;
 
 struct AttnArgs {
   PagedBatch b;
@@ -557,13 +559,18 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const Row& row, int hg
     qf[st] = row.ok ? *reinterpret_cast<const u32x4_t*>(q + 16 * st + 8 * hg) : u32x4_t{0u, 0u, 0u, 0u};
 }
 
+// Whether a tile of `count` blocks has one part, which then writes out itself.
+__device__ __forceinline__ bool one_part(const AttnArgs& a, int count) {
+  return a.parts == 1 || (kTree && count <= a.part_blocks);
+}
+
 // The lane's share of its row, finished or as a part: o[t][4 j + i] = O[32 t +
 // 8 j + 4 h + i].
 template <int DH>
 __device__ __forceinline__ void store_row(const AttnArgs& a, const Row& row, const RowState<DH>& st, float l,
-                                          int hg, int part) {
+                                          int hg, int part, bool whole) {
   if (!row.ok) return;
-  if (a.parts > 1) {
+  if (!whole) {
     const long at = row.part * a.parts + part;
     if (hg == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(st.t, l);
     float* o = a.ws_o + at * DH;
@@ -595,8 +602,20 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Row& row, con
 // the eight XCDs in turn, so the tiles of one head meet in one L2.  Then the
 // tiles, and the parts slowest: short sequences have the first parts only, which
 // must not all fall to the same XCDs.
+// kTree: the four tiles of a run go to one XCD one after the other, where they read
+// the same keys (a tree's rows times the heads that share its keys are several
+// tiles); then the heads, the parts, turned on by one with every run, and the runs.
+// (64 nodes on 131000 keys, 16 heads of 128 on 2: 97 us, dealt out as above 151.)
 __device__ __forceinline__ void work_item(const AttnArgs& a, int& tile, int& hk, int& part) {
   const unsigned w = a.first + blockIdx.x;
+  if constexpr (kTree) {
+    const unsigned unit = w % kXcds + w / (kXcds * kTileRun) * kXcds;
+    const unsigned r = unit / a.b.n_heads, run = r / a.parts;
+    hk = unit - r * a.b.n_heads;
+    part = (r - run * a.parts + run) % a.parts;
+    tile = run * kTileRun + w / kXcds % kTileRun;
+    return;
+  }
   hk = w % a.b.n_heads;
   const unsigned r = w / a.b.n_heads;
   part = r / a.tiles;
@@ -659,6 +678,7 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
   __shared__ uint64_t nodes[kTree ? 32 * kWaves : 1][kTreeWords];
   int tile_no, hk, part;
   work_item(a, tile_no, hk, part);
+  if (kTree && tile_no >= a.tiles) return;
   const Tile tile = find_tile_longest_first(a, tile_no);
   if (tile.n <= 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -745,7 +765,7 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
   }
   const float l = st.l + __shfl_xor(st.l, 32, 64);
   st.t = mark_seen<KB>(a, tile.s, blocks, from, to, 1, row, l, pages, st.t);
-  store_row<DH>(a, row, st, l, hg, part);
+  store_row<DH>(a, row, st, l, hg, part, one_part(a, blocks.count));
 }
 
 // 32 rows; wave w takes blocks w, w + 4, ... of 32 keys.  The keys go from
@@ -767,6 +787,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   __shared__ uint64_t nodes[kTree ? 32 * kWaves : 1][kTreeWords];
   int tile_no, hk, part;
   work_item(a, tile_no, hk, part);
+  if (kTree && tile_no >= a.tiles) return;
   const Tile tile = find_tile(a, tile_no);
   if (tile.n <= 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -873,7 +894,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
         }
     }
   }
-  if (wave == 0) store_row<DH>(a, row, st, l, hg, part);
+  if (wave == 0) store_row<DH>(a, row, st, l, hg, part, one_part(a, blocks.count));
 }
 
 // ---------------------------------------------------------------------------
@@ -896,6 +917,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
   __shared__ uint64_t nodes[kTree ? kWaves : 1][kTree ? 16 * QT : 1][kTreeWords];
   int tile_no, hk, part;
   work_item(a, tile_no, hk, part);
+  if (kTree && tile_no >= a.tiles) return;
   const Tile tile = find_tile(a, tile_no);
   if (tile.n <= 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1093,7 +1115,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
       l = fmaf(part_l[w][i], f[w], l);
     }
     const Row mine = make_row(a, tile, hk, 16 * qt + i);
-    const bool last = a.parts == 1;
+    const bool last = one_part(a, blocks.count);
     const float inv = last ? inverse_sum(l, m) : 1.f;
     const long slot = mine.part * a.parts + part;
     float* out = last ? static_cast<float*>(a.out) + mine.out_at : a.ws_o + slot * DH;
@@ -1133,6 +1155,7 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int r
   if (share * rows >= t.n) return;
   const int count = tile_blocks(a, t, kb).count;
   const int parts = max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
+  if (kTree && parts == 1) return;
   const int octet = threadIdx.x >> 3, subs = 32 / rows;  // octets of a row
   const int sub = octet % subs;
   for (int row0 = share * rows; row0 < t.n; row0 += shares * rows) {
@@ -1204,6 +1227,13 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   p.kind = dtype == DT_F32 ? F32
            : packed <= 48l * b.n_seqs || (packed <= 96l * b.n_seqs && few <= 512) ? FEW
                                                                                   : MANY;
+  // Trees: tiles of 32 rows while what all of them read together, at max_kv keys
+  // each, is at most 256 MB.  More of it costs more than the 128-row tiles' longer way
+  // through a block (one tree of 128 nodes on 8000 keys, 16 heads of 64: 25 us, tiles
+  // of 128: 40; 32 of 2 nodes on 500 to 8000, 32 heads of 128 on 4: 44 and 66; of 4: 69
+  // and 66; one of 20 on 131000, 16 heads on 2: 112 and 91; 32 of 40 on 8000: 456 and
+  // 285).
+  if (kTree && p.kind != F32) p.kind = few * b.max_kv * b.d_head <= 1l << 26 ? FEW : MANY;
   // fp32: 32 rows to a tile read the keys half as often, where that still makes
   // tiles enough (500 rows in each of 4 sequences, 3500 keys, 16 heads of 64: 365
   // us, tiles of 16: 440; 377 rows in 5 sequences, 12 heads: 25 and 17).
@@ -1230,6 +1260,13 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   long parts = std::min<long>((fill + items - 1) / items, blocks / (p.kind == MANY ? 4 : 8));
   const long even = std::min<long>((4096 + items - 1) / items, static_cast<long>(blocks) * p.kb / 1024);
   if (p.kind != MANY && even >= 4) parts = std::max(parts, even);
+  // Trees, 128 rows to a tile: two workgroups for every CU, and parts of at most 2560
+  // keys, where sequences may differ in length (32 trees of 17 to 63 nodes on 530 to
+  // 7700 keys, 32 heads of 128 on 4: 101 us, undivided 218, with 1024 keys to a part
+  // 133; 4 trees of 64 on 20000: 106, twice as many parts 122).
+  if (kTree && p.kind == MANY)
+    parts = std::min({std::max<long>(512 / items, (blocks + 39) / 40), static_cast<long>(blocks) / 8,
+                      std::max(4096 / items, 1l)});
   parts = std::max(parts, 1l);
   const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
   parts = std::max(1l, std::min<long>(parts, static_cast<long>(ws_bytes / per_part)));
@@ -1292,7 +1329,11 @@ hipError_t run_attention(int dtype, const PagedBatch& b, int m, int heads_q, con
     a.ws_o = static_cast<float*>(ws);
     a.ws_ml = a.ws_o + static_cast<size_t>(p.parts) * m * heads_q * b.d_head;
   }
-  const long grid = static_cast<long>(p.tiles) * p.parts * b.n_heads;
+  long grid = static_cast<long>(p.tiles) * p.parts * b.n_heads;
+  if (kTree) {
+    const long units = static_cast<long>((p.tiles + kTileRun - 1) / kTileRun) * p.parts * b.n_heads;
+    grid = (units + kXcds - 1) / kXcds * kXcds * kTileRun;
+  }
   for (long first = 0; first < grid; first += kMaxGrid) {
     a.first = static_cast<unsigned>(first);
     const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, grid - first)));
