@@ -35,13 +35,16 @@ __device__ __forceinline__ void better(float& v, int& i, float v2, int i2) {
 // ---------------------------------------------------------------------------
 // p = exp((x - max) / T) / sum, a workgroup to a row; T 0: one at the first
 // maximum.
+//
+// Bound by reading the logits and writing fp32: the first HELD x THREADS sixteen-byte
+// pieces of a row stay in registers between the passes, so that it is read once
+// (600 rows of 65536 in bf16, 236 MB: 56 us, 4.2 TB/s; read twice 68; with streaming
+// stores 80); what a longer row has beyond them is read again.
 // ---------------------------------------------------------------------------
-constexpr int kProbThreads = 1024;
-
-template <typename T>
-__global__ __launch_bounds__(kProbThreads) void probabilities(const T* logits, long ld, const float* temperature,
-                                                              int first, int vocab, float* out, long ld_out) {
-  constexpr int N = kPer<T>, WAVES = kProbThreads / 64;
+template <typename T, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void probabilities(const T* logits, long ld, const float* temperature, int first,
+                                                         int vocab, float* out, long ld_out) {
+  constexpr int N = kPer<T>, WAVES = THREADS / 64;
   __shared__ float sm[WAVES], ss[WAVES];
   __shared__ int si[WAVES];
   const long row = static_cast<long>(first) + blockIdx.x;
@@ -50,105 +53,130 @@ __global__ __launch_bounds__(kProbThreads) void probabilities(const T* logits, l
   const float temp = temperature ? temperature[row] : 1.f;
   const bool cold = !(temp > kCold);
   const float scale = cold ? 0.f : kLog2e / temp;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, whole = vocab / N;
-  // a finite reference of no values: -infinity weighs 0 against it
-  float top = cold ? -kInf : kLowest, sum = 0.f;
-  int at = vocab;
-  auto take = [&](const float* v, int n, int i0) {
-    if (cold) {
-      for (int e = 0; e < n; ++e) {
-        at = v[e] > top ? i0 + e : at;
-        top = fmaxf(top, v[e]);
-      }
-      return;
-    }
-    float m = top;
-    for (int e = 0; e < n; ++e) m = fmaxf(m, v[e]);
-    sum *= __builtin_amdgcn_exp2f((top - m) * scale);
-    for (int e = 0; e < n; ++e) sum += __builtin_amdgcn_exp2f((v[e] - m) * scale);
-    top = m;
-  };
-  for (int g = threadIdx.x; g < whole; g += kProbThreads) {
-    float v[N];
-    unpack16(load_any(x + N * g), v, static_cast<const T*>(nullptr));
-    take(v, N, N * g);
-  }
-  if (N * whole + static_cast<int>(threadIdx.x) < vocab) {
-    const int i = N * whole + threadIdx.x;
-    const float v = load_one(x + i);
-    take(&v, 1, i);
-  }
+  const int wave = threadIdx.x >> 6, whole = vocab / N, tid = threadIdx.x;
+  // the piece g of the row, v[0 .. n) its elements
+  u32x4_t held[HELD];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(top, o, 64), s2 = __shfl_xor(sum, o, 64);
-    const int i2 = __shfl_xor(at, o, 64);
-    const float m = fmaxf(top, m2);
-    sum = sum * __builtin_amdgcn_exp2f((top - m) * scale) + s2 * __builtin_amdgcn_exp2f((m2 - m) * scale);
-    better(top, at, m2, i2);
-  }
-  if (lane == 0) {
-    sm[wave] = top;
-    ss[wave] = sum;
-    si[wave] = at;
-  }
-  __syncthreads();
-  top = sm[0];
-  at = si[0];
-  for (int w = 1; w < WAVES; ++w) better(top, at, sm[w], si[w]);
-  sum = 0.f;
-  for (int w = 0; w < WAVES; ++w)
-    sum += ss[w] * __builtin_amdgcn_exp2f((sm[w] - top) * scale);
-  const float inv = 1.f / sum;
-  auto p_of = [&](float v, int i) {
-    return cold ? (i == at ? 1.f : 0.f) : __builtin_amdgcn_exp2f((v - top) * scale) * inv;
+  for (int k = 0; k < HELD; ++k)
+    if (tid + k * THREADS < whole) held[k] = load_any(x + N * (tid + k * THREADS));
+  const int odd = N * whole + tid;  // the row's last, single elements
+  const float alone = odd < vocab ? load_one(x + odd) : 0.f;
+  auto each = [&](auto&& take) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      const int g = tid + k * THREADS;
+      if (g >= whole) continue;
+      float v[N];
+      unpack16(held[k], v, static_cast<const T*>(nullptr));
+      take(v, N * g);
+    }
+    for (int g = tid + HELD * THREADS; g < whole; g += THREADS) {
+      float v[N];
+      unpack16(load_any(x + N * g), v, static_cast<const T*>(nullptr));
+      take(v, N * g);
+    }
   };
-  for (int g = threadIdx.x; g < whole; g += kProbThreads) {
-    float v[N];
-    unpack16(load_any(x + N * g), v, static_cast<const T*>(nullptr));
+  if (cold) {
+    float top = -kInf;
+    int at = vocab;
+    auto take = [&](float v, int i) {
+      at = v > top ? i : at;
+      top = fmaxf(top, v);
+    };
+    each([&](const float* v, int i) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) take(v[e], i + e);
+    });
+    if (odd < vocab) take(alone, odd);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) better(top, at, __shfl_xor(top, o, 64), __shfl_xor(at, o, 64));
+    if ((tid & 63) == 0) {
+      sm[wave] = top;
+      si[wave] = at;
+    }
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) better(top, at, sm[w], si[w]);
+    for (int g = tid; g < vocab / 4; g += THREADS) {
+      any_f32x4_t o;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = 4 * g + k == at ? 0x3F800000u : 0u;
+      *reinterpret_cast<any_f32x4_t*>(y + 4 * g) = o;
+    }
+    if (vocab / 4 * 4 + tid < vocab) y[vocab / 4 * 4 + tid] = vocab / 4 * 4 + tid == at ? 1.f : 0.f;
+    return;
+  }
+  float top = kLowest;  // finite, so that -infinity weighs 0 against it
+  each([&](const float* v, int) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = fmaxf(top, v[e]);
+  });
+  if (odd < vocab) top = fmaxf(top, alone);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if ((tid & 63) == 0) sm[wave] = top;
+  __syncthreads();
+  for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm[w]);
+  auto weight = [&](float v) { return __builtin_amdgcn_exp2f((v - top) * scale); };
+  float sum = 0.f;
+  each([&](const float* v, int) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum += weight(v[e]);
+  });
+  if (odd < vocab) sum += weight(alone);
+  sum = wave_sum(sum);
+  if ((tid & 63) == 0) ss[wave] = sum;
+  __syncthreads();
+  sum = 0.f;
+  for (int w = 0; w < WAVES; ++w) sum += ss[w];
+  const float inv = 1.f / sum;
+  each([&](const float* v, int i) {
 #pragma unroll
     for (int e = 0; e < N; e += 4) {
       any_f32x4_t o;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(p_of(v[e + k], N * g + e + k));
-      *reinterpret_cast<any_f32x4_t*>(y + N * g + e) = o;
+      for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(weight(v[e + k]) * inv);
+      *reinterpret_cast<any_f32x4_t*>(y + i + e) = o;
     }
-  }
-  if (N * whole + static_cast<int>(threadIdx.x) < vocab) {
-    const int i = N * whole + threadIdx.x;
-    y[i] = p_of(load_one(x + i), i);
-  }
+  });
+  if (odd < vocab) y[odd] = weight(alone) * inv;
 }
 
 // ---------------------------------------------------------------------------
-// Greedy verification: the first maximum of every row.
+// Greedy verification: the first maximum of every row.  Bound by reading them.
 // ---------------------------------------------------------------------------
+constexpr int kBestThreads = 512;
+
 template <typename T>
-__global__ __launch_bounds__(256) void row_best(const T* p, long ld, int first, int vocab, int32_t* best) {
-  constexpr int N = kPer<T>;
-  __shared__ float sm[4];
-  __shared__ int si[4];
+__global__ __launch_bounds__(kBestThreads) void row_best(const T* p, long ld, int first, int vocab, int32_t* best) {
+  constexpr int N = kPer<T>, WAVES = kBestThreads / 64, AHEAD = 8;
+  __shared__ float sm[WAVES];
+  __shared__ int si[WAVES];
   const long row = static_cast<long>(first) + blockIdx.x;
   const T* x = p + row * ld;
   float top = -kInf;
   int at = vocab;
   const int whole = vocab / N;
-  for (int g = threadIdx.x; g < whole; g += 256) {
-    float v[N];
-    unpack16(load_any(x + N * g), v, static_cast<const T*>(nullptr));
+  auto take = [&](float v, int i) {
+    at = v > top ? i : at;
+    top = fmaxf(top, v);
+  };
+  for (int g0 = threadIdx.x; g0 < whole; g0 += AHEAD * kBestThreads) {
+    u32x4_t x16[AHEAD];
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (v[e] > top) {
-        top = v[e];
-        at = N * g + e;
-      }
+    for (int k = 0; k < AHEAD; ++k)
+      x16[k] = load_any(x + static_cast<long>(N) * min(g0 + k * kBestThreads, whole - 1));
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int g = min(g0 + k * kBestThreads, whole - 1);  // the last one again changes nothing
+      float v[N];
+      unpack16(x16[k], v, static_cast<const T*>(nullptr));
+#pragma unroll
+      for (int e = 0; e < N; ++e) take(v[e], N * g + e);
+    }
   }
   if (N * whole + static_cast<int>(threadIdx.x) < vocab) {
     const int i = N * whole + threadIdx.x;
-    const float v = load_one(x + i);
-    if (v > top) {
-      top = v;
-      at = i;
-    }
+    take(load_one(x + i), i);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) better(top, at, __shfl_xor(top, o, 64), __shfl_xor(at, o, 64));
@@ -158,13 +186,13 @@ __global__ __launch_bounds__(256) void row_best(const T* p, long ld, int first, 
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < 4; ++w) better(top, at, sm[w], si[w]);
+    for (int w = 1; w < WAVES; ++w) better(top, at, sm[w], si[w]);
     best[row] = at < vocab ? at : -1;
   }
 }
 
 // ---------------------------------------------------------------------------
-// The walk down a tree, and the token after it: a workgroup to a sequence.
+// The walk down a tree, and the token after it.
 //
 // cur starts at node 0, and the nodes are looked at in ascending order, those
 // whose parent is cur; an accepted one becomes cur.  Without probabilities of
@@ -175,140 +203,320 @@ __global__ __launch_bounds__(256) void row_best(const T* p, long ld, int first, 
 // max(alpha p - beta q, 0) loses what is left in the difference of two products
 // that grow with every rejection).  All of it in fp64: the sums decide between
 // tokens.
+//
+// What the walk asks of p and q are single values, one to a node, which the lanes
+// of a wave fetch for all nodes at once; it then runs in registers.  Only a
+// rejection that leaves other children (drawn ones) needs a sum over the
+// vocabulary on the way; the last one's, and the sum that the next token is drawn
+// from, are taken by many workgroups:
+//   verify_walk   drawn tokens: the walk, a workgroup to a sequence
+//   verify_sums   sums of kTile weights each, a wave to a tile; without a draft
+//                 each workgroup repeats the walk, which costs less than a launch
+//   verify_pick   the tile that the random number falls into, and the token in it,
+//                 a wave to a sequence
+// Bound by the chain of dependent loads of each: TIMES.
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
+constexpr int kWalkThreads = 1024;
+constexpr int kSumThreads = 256;
 constexpr int kTile = 1024;  // tokens of which a wave sums the weights
-constexpr int kMaxTiles = kMaxVocab / kTile;
 constexpr int kPart = kTile / 64;
 constexpr int kMaxNodes = 256;
+constexpr int kChunks = kMaxNodes / 64;
 
 // Values that are no probabilities (negative, infinite, NaN) count as 0.
 __device__ __forceinline__ float proper(float x) { return x > 0.f && x < kInf ? x : 0.f; }
 
-// A sequence's tree: its first kMaxNodes rows [row0, row0 + n), bounded by the m rows.
-struct Tree {
-  int row0, n, rows;           // nodes; rows of the sequence in all
-  const int32_t* parent;       // LDS [n], -1: none
-  const int32_t* token;        // LDS [n]
+// A sequence's rows [row0, row0 + rows), bounded by the m rows; the first kMaxNodes
+// are nodes.
+struct TreeRows {
+  int row0, rows, n;
 };
-__device__ __forceinline__ Tree tree_of(const VerifyArgs& a, int s, int32_t* parent, int32_t* token) {
-  Tree t;
+__device__ __forceinline__ TreeRows tree_rows(const VerifyArgs& a, int s) {
+  TreeRows t;
   t.row0 = min(max(a.q_start[s], 0), a.m);
   t.rows = max(min(max(a.q_start[s + 1], 0), a.m) - t.row0, 0);
   t.n = min(t.rows, kMaxNodes);
-  t.parent = parent;
-  t.token = token;
-  for (int i = threadIdx.x; i < t.n; i += blockDim.x) {
-    const int p = a.parent[t.row0 + i];
-    parent[i] = p >= 0 && p < i ? p : -1;
-    token[i] = a.tokens[t.row0 + i];
-  }
   return t;
 }
 
-template <typename T>
+// Node 64 c + lane in element c: its parent (-1: none), token, random number, and p
+// and q of the token in the parent's rows.
+struct Nodes {
+  int parent[kChunks], token[kChunks];
+  float r[kChunks], p[kChunks], q[kChunks];
+};
+__device__ __forceinline__ void load_parents(const VerifyArgs& a, const TreeRows& t, Nodes& d) {
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    d.parent[c] = d.token[c] = -1;
+    const int i = 64 * c + static_cast<int>(threadIdx.x & 63);
+    if (i < t.n) {
+      const int up = a.parent[t.row0 + i];
+      d.parent[c] = up >= 0 && up < i ? up : -1;
+      d.token[c] = a.tokens[t.row0 + i];
+    }
+  }
+}
+template <typename T, bool DRAWN>
+__device__ __forceinline__ void load_nodes(const VerifyArgs& a, const TreeRows& t, Nodes& d) {
+  load_parents(a, t, d);
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int i = 64 * c + static_cast<int>(threadIdx.x & 63);
+    d.r[c] = d.p[c] = d.q[c] = 0.f;
+    if (i >= t.n) continue;
+    d.r[c] = a.random[t.row0 + i];
+    if (d.parent[c] < 0 || d.token[c] < 0 || d.token[c] >= a.vocab) continue;
+    const long row = t.row0 + d.parent[c];
+    d.p[c] = proper(load_one(static_cast<const T*>(a.p) + row * a.ld_p + d.token[c]));
+    if (DRAWN) d.q[c] = proper(load_one(static_cast<const T*>(a.draft) + row * a.ld_draft + d.token[c]));
+  }
+}
+__device__ __forceinline__ int of_node(const int (&v)[kChunks], int i) {
+  int x = __builtin_amdgcn_readlane(v[0], i & 63);
+#pragma unroll
+  for (int c = 1; c < kChunks; ++c)
+    if (i >> 6 == c) x = __builtin_amdgcn_readlane(v[c], i & 63);
+  return x;
+}
+__device__ __forceinline__ float of_node(const float (&v)[kChunks], int i) {
+  int bits[kChunks];
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) bits[c] = __float_as_int(v[c]);
+  return __int_as_float(of_node(bits, i));
+}
+// The next child of `node` behind node `after` (kMaxNodes: none).
+__device__ __forceinline__ int next_child(const Nodes& d, int node, int after) {
+  int found = kMaxNodes;
+#pragma unroll
+  for (int c = kChunks - 1; c >= 0; --c) {
+    const int i = 64 * c + static_cast<int>(threadIdx.x & 63);
+    const uint64_t who = __builtin_amdgcn_ballot_w64(d.parent[c] == node && i > after);
+    if (who) found = 64 * c + __builtin_ctzll(who);
+  }
+  return found;
+}
+// Whether token x has hung on `node` before node i.
+__device__ __forceinline__ bool had_child(const Nodes& d, int node, int i, int x) {
+  uint64_t who = 0;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int j = 64 * c + static_cast<int>(threadIdx.x & 63);
+    who |= __builtin_amdgcn_ballot_w64(d.parent[c] == node && j < i && d.token[c] == x);
+  }
+  return who != 0;
+}
+
+// Weights of the tokens after a node: p, and q (null: none) as `rejected` sums W (LDS;
+// the first is 1) leave it.
+template <typename T, bool DRAWN>
 struct Weights {
   const T* p;
-  const T* q;         // null: none
-  const double* sums; // LDS: W of every rejection so far
+  const T* q;
+  const double* sums;
   int rejected;
   __device__ __forceinline__ double of(float pv, float qv) const {
-    double v = proper(pv);
-    if (q) {
-      const double d = proper(qv);
-      if (rejected > 0) v = fmax(v - d, 0.0);  // W of the first is 1
+    double v = pv;
+    if constexpr (DRAWN) {
+      const double d = qv;
+      if (rejected > 0) v = fmax(v - d, 0.0);
       for (int k = 1; k < rejected; ++k) v = fmax(v / sums[k] - d, 0.0);
     }
     return v;
   }
-  __device__ __forceinline__ double at(int i) const { return of(load_one(p + i), q ? load_one(q + i) : 0.f); }
 };
-
-// The next child of `node` behind node `after` (t.n: none); all lanes of the wave.
-__device__ __forceinline__ int next_child(const Tree& t, int node, int after) {
-  for (int i0 = (after + 1) & ~63; i0 < t.n; i0 += 64) {
-    const int i = i0 + static_cast<int>(threadIdx.x & 63);
-    const uint64_t who = __builtin_amdgcn_ballot_w64(i > after && i < t.n && t.parent[min(i, t.n - 1)] == node);
-    if (who) return i0 + __builtin_ctzll(who);
-  }
-  return t.n;
-}
-// Whether token x has hung on `node` before node i.
-__device__ __forceinline__ bool had_child(const Tree& t, int node, int i, int x) {
-  for (int j0 = 0; j0 < i; j0 += 64) {
-    const int j = j0 + static_cast<int>(threadIdx.x & 63);
-    if (__builtin_amdgcn_ballot_w64(j < i && t.parent[min(j, t.n - 1)] == node && t.token[min(j, t.n - 1)] == x))
-      return true;
-  }
-  return false;
+template <typename T, bool DRAWN>
+__device__ __forceinline__ Weights<T, DRAWN> weights_of(const VerifyArgs& a, const TreeRows& t, int node, int rejected,
+                                                        const double* sums) {
+  const long row = t.row0 + node;
+  return Weights<T, DRAWN>{static_cast<const T*>(a.p) + row * a.ld_p,
+                           DRAWN ? static_cast<const T*>(a.draft) + row * a.ld_draft : nullptr, sums, rejected};
 }
 
-// The weights of a tile's tokens 16 to a lane, in order; tokens of node's children are 0
-// where the weights have no q.
-template <typename T>
-__device__ __forceinline__ void tile_weights(const VerifyArgs& a, const Tree& t, int node, const Weights<T>& w,
-                                             int tile, double (&v)[kPart]) {
+// Tokens without weight: those that the children of the final node proposed.
+struct Out {
+  int32_t* token;  // LDS [kMaxNodes]
+  int n;
+};
+// `write`: this wave fills the list.
+__device__ __forceinline__ Out list_children(const Nodes& d, int node, int32_t* token, bool write) {
+  Out o{token, 0};
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const bool mine = d.parent[c] == node;
+    const uint64_t who = __builtin_amdgcn_ballot_w64(mine);
+    if (mine && write) token[o.n + __builtin_popcountll(who & ((uint64_t{1} << lane) - 1))] = d.token[c];
+    o.n += __builtin_popcountll(who);
+  }
+  return o;
+}
+
+// The weights of a tile's tokens, 16 to a lane, in order.
+template <typename T, bool DRAWN>
+__device__ __forceinline__ void tile_weights(int vocab, const Weights<T, DRAWN>& w, const Out& out, int tile,
+                                             double (&v)[kPart]) {
   constexpr int N = kPer<T>;
   const int lane = threadIdx.x & 63, i0 = tile * kTile + lane * kPart;
-  float pv[kPart], qv[kPart];
-  if (i0 + kPart <= a.vocab) {
+  float pv[kPart], qv[kPart] = {};
+  if (i0 + kPart <= vocab) {
 #pragma unroll
     for (int k = 0; k < kPart; k += N) {
       unpack16(load_any(w.p + i0 + k), pv + k, static_cast<const T*>(nullptr));
-      if (w.q) unpack16(load_any(w.q + i0 + k), qv + k, static_cast<const T*>(nullptr));
+      if (DRAWN) unpack16(load_any(w.q + i0 + k), qv + k, static_cast<const T*>(nullptr));
     }
   } else {
 #pragma unroll
     for (int k = 0; k < kPart; ++k) {
-      pv[k] = i0 + k < a.vocab ? load_one(w.p + i0 + k) : 0.f;
-      qv[k] = w.q && i0 + k < a.vocab ? load_one(w.q + i0 + k) : 0.f;
+      pv[k] = i0 + k < vocab ? load_one(w.p + i0 + k) : 0.f;
+      if (DRAWN) qv[k] = i0 + k < vocab ? load_one(w.q + i0 + k) : 0.f;
     }
   }
 #pragma unroll
-  for (int k = 0; k < kPart; ++k) v[k] = w.of(pv[k], w.q ? qv[k] : 0.f);
-  if (w.q) return;
-  for (int j0 = 1; j0 < t.n; j0 += 64) {
-    const int j = j0 + lane;
-    int x = -1;
-    if (j < t.n && t.parent[j] == node) x = t.token[j];
-    uint64_t who = __builtin_amdgcn_ballot_w64(x >= 0 && x / kTile == tile);
-    for (; who; who &= who - 1) {
-      const int out = __builtin_amdgcn_readlane(x, __builtin_ctzll(who)) - i0;
+  for (int k = 0; k < kPart; ++k) v[k] = w.of(proper(pv[k]), proper(qv[k]));
+  if (DRAWN) return;
+  for (int j0 = 0; j0 < out.n; j0 += 64) {
+    const int x = j0 + lane < out.n ? out.token[j0 + lane] : -1;
+    for (uint64_t who = __builtin_amdgcn_ballot_w64(x >= 0 && x / kTile == tile); who; who &= who - 1) {
+      const int at = __builtin_amdgcn_readlane(x, __builtin_ctzll(who)) - i0;
 #pragma unroll
       for (int k = 0; k < kPart; ++k)
-        if (k == out) v[k] = 0.0;
+        if (k == at) v[k] = 0.0;
     }
   }
 }
-
-// Sums of every tile into LDS, and their total (in order) to all threads.
-template <typename T>
-__device__ __forceinline__ double sum_tiles(const VerifyArgs& a, const Tree& t, int node, const Weights<T>& w,
-                                            double* sums, double* total) {
-  const int tiles = (a.vocab + kTile - 1) / kTile;
-  __syncthreads();
-  for (int tile = threadIdx.x >> 6; tile < tiles; tile += kWaves) {
-    double v[kPart], sum = 0.0;
-    tile_weights(a, t, node, w, tile, v);
+template <typename T, bool DRAWN>
+__device__ __forceinline__ double tile_sum(int vocab, const Weights<T, DRAWN>& w, const Out& out, int tile) {
+  double v[kPart], sum = 0.0;
+  tile_weights(vocab, w, out, tile, v);
 #pragma unroll
-    for (int k = 0; k < kPart; ++k) sum += v[k];
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) sums[tile] = sum;
-  }
-  __syncthreads();
-  if (threadIdx.x < 64) {
-    double mine = 0.0;
-    const int per = (tiles + 63) / 64;
-    for (int k = 0; k < per; ++k) {
-      const int i = threadIdx.x * per + k;
-      mine += i < tiles ? sums[i] : 0.0;
+  for (int k = 0; k < kPart; ++k) sum += v[k];
+  return wave_sum(sum);
+}
+
+// How a walk ended.
+struct End {
+  int node, kept;
+  int rejected;  // drawn: rejections of node's children, the last one's sum not taken
+};
+
+// The walk, by every wave of the workgroup; the kept nodes go to `line` (LDS) if `write`.
+// more(weights): the sum of the weights over the vocabulary.  sums: LDS, W of each rejection.
+template <typename T, bool DRAWN, typename Sum>
+__device__ __forceinline__ End walk(const VerifyArgs& a, const TreeRows& t, const Nodes& d, int32_t* line, bool write,
+                                    double* sums, Sum&& sum_of) {
+  End e{0, 1, 0};
+  double W = 1.0;
+  if (write) line[0] = 0;
+  for (int i = next_child(d, 0, 0); i < kMaxNodes;) {
+    const Weights<T, DRAWN> w = weights_of<T, DRAWN>(a, t, e.node, e.rejected, sums);
+    const float qx = of_node(d.q, i);
+    double wx = w.of(of_node(d.p, i), qx);
+    if (!DRAWN && had_child(d, e.node, i, of_node(d.token, i))) wx = 0.0;
+    const double r = of_node(d.r, i);
+    if (DRAWN ? r * static_cast<double>(qx) * W < wx : r * W < wx) {
+      e.node = i;
+      if (write) line[e.kept] = i;
+      ++e.kept;
+      e.rejected = 0;
+      W = 1.0;
+      i = next_child(d, e.node, i);
+      continue;
     }
-    mine = wave_sum(mine);
-    if (threadIdx.x == 0) *total = mine;
+    i = next_child(d, e.node, i);
+    if constexpr (DRAWN) {
+      if (write) sums[e.rejected] = W;
+      ++e.rejected;
+      if (i < kMaxNodes) {
+        const double sum = sum_of(weights_of<T, DRAWN>(a, t, e.node, e.rejected, sums));
+        if (sum > 0.0)
+          W = sum;
+        else
+          --e.rejected;
+      }
+    } else {
+      W -= wx;
+    }
   }
+  return e;
+}
+
+__device__ __forceinline__ void store_path(const VerifyArgs& a, const TreeRows& t, int s, const End& e,
+                                           const int32_t* line) {
+  for (int i = threadIdx.x; i < t.rows; i += blockDim.x) a.path[t.row0 + i] = i < e.kept ? line[i] : -1;
+  if (threadIdx.x == 0) a.kept[s] = t.n > 0 ? e.kept : 0;
+}
+
+// What the kernels leave for each other, one to a sequence.
+struct Header {
+  int node, rejected;
+  double sums[kMaxNodes];
+};
+
+template <typename T>
+__global__ __launch_bounds__(kWalkThreads) void verify_walk(const VerifyArgs a, Header* headers) {
+  __shared__ double sums[kMaxNodes], part[kWalkThreads / 64];
+  __shared__ int32_t line[kMaxNodes];
+  const int s = blockIdx.x, wave = threadIdx.x >> 6;
+  const TreeRows t = tree_rows(a, s);
+  Nodes d;
+  load_nodes<T, true>(a, t, d);
+  const int tiles = (a.vocab + kTile - 1) / kTile;
+  const End e = walk<T, true>(a, t, d, line, threadIdx.x == 0, sums, [&](const Weights<T, true>& w) {
+    __syncthreads();  // W of the rejection is there, the sums before are read
+    double sum = 0.0;
+    for (int tile = wave; tile < tiles; tile += kWalkThreads / 64) sum += tile_sum(a.vocab, w, Out{nullptr, 0}, tile);
+    if ((threadIdx.x & 63) == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int k = 0; k < kWalkThreads / 64; ++k) sum += part[k];
+    return sum;
+  });
   __syncthreads();
-  return *total;
+  store_path(a, t, s, e, line);
+  Header* h = headers + s;
+  for (int k = threadIdx.x; k < e.rejected; k += kWalkThreads) h->sums[k] = sums[k];
+  if (threadIdx.x == 0) {
+    h->node = e.node;
+    h->rejected = e.rejected;
+  }
+}
+
+template <typename T, bool DRAWN>
+__global__ __launch_bounds__(kSumThreads) void verify_sums(const VerifyArgs a, Header* headers, double* tile_sums,
+                                                           int shares) {
+  __shared__ double sums[DRAWN ? kMaxNodes : 1];
+  __shared__ int32_t line[kMaxNodes], children[kMaxNodes];
+  const int s = blockIdx.x / shares, share = blockIdx.x % shares;
+  const TreeRows t = tree_rows(a, s);
+  Header* h = headers + s;
+  int node, rejected = 0;
+  Out out{children, 0};
+  if constexpr (DRAWN) {
+    if (t.n == 0) return;
+    node = h->node;
+    rejected = h->rejected;
+    for (int k = threadIdx.x; k < rejected; k += kSumThreads) sums[k] = h->sums[k];
+    __syncthreads();
+  } else {
+    Nodes d;
+    load_nodes<T, false>(a, t, d);
+    const End e = walk<T, false>(a, t, d, line, threadIdx.x == 0, sums, [](const Weights<T, false>&) { return 0.0; });
+    out = list_children(d, e.node, children, threadIdx.x < 64);
+    node = e.node;
+    __syncthreads();
+    if (share == 0) {
+      store_path(a, t, s, e, line);
+      if (threadIdx.x == 0) h->node = node;
+    }
+    if (t.n == 0) return;
+  }
+  const Weights<T, DRAWN> w = weights_of<T, DRAWN>(a, t, node, rejected, sums);
+  const int tiles = (a.vocab + kTile - 1) / kTile;
+  for (int tile = share * (kSumThreads / 64) + (threadIdx.x >> 6); tile < tiles; tile += shares * (kSumThreads / 64)) {
+    const double sum = tile_sum(a.vocab, w, out, tile);
+    if ((threadIdx.x & 63) == 0) tile_sums[static_cast<long>(s) * tiles + tile] = sum;
+  }
 }
 
 // v summed over the lanes up to and with this one.
@@ -322,17 +530,19 @@ __device__ __forceinline__ double scan_add(double v) {
   return v;
 }
 
-// The first token at which the summed weights pass `goal`, given the tiles' sums; the
-// last one with a weight if none does, -1 if none has any.  One wave.
-template <typename T>
-__device__ __forceinline__ int pick(const VerifyArgs& a, const Tree& t, int node, const Weights<T>& w,
-                                    const double* sums, double goal) {
-  const int tiles = (a.vocab + kTile - 1) / kTile, lane = threadIdx.x & 63;
-  double before = 0.0;
+// The first token at which the summed weights pass r times their sum, given the tiles'
+// sums; the last one with a weight if none does.  -1 if none has any.
+template <typename T, bool DRAWN>
+__device__ __forceinline__ int pick(int vocab, const Weights<T, DRAWN>& w, const Out& out, const double* tile_sums,
+                                    double r) {
+  const int tiles = (vocab + kTile - 1) / kTile, lane = threadIdx.x & 63;
+  double total = 0.0;
+  for (int i = lane; i < tiles; i += 64) total += tile_sums[i];
+  const double goal = r * wave_sum(total);
+  double before = 0.0, last_before = 0.0;
   int tile = -1, last = -1;
-  double last_before = 0.0;
   for (int i0 = 0; i0 < tiles && tile < 0; i0 += 64) {
-    const double mine = i0 + lane < tiles ? sums[i0 + lane] : 0.0;
+    const double mine = i0 + lane < tiles ? tile_sums[i0 + lane] : 0.0;
     const double upto = before + scan_add(mine);
     const uint64_t over = __builtin_amdgcn_ballot_w64(mine > 0.0 && upto > goal);
     const uint64_t some = __builtin_amdgcn_ballot_w64(mine > 0.0);
@@ -355,7 +565,7 @@ __device__ __forceinline__ int pick(const VerifyArgs& a, const Tree& t, int node
     before = last_before;
   }
   double v[kPart], mine = 0.0;
-  tile_weights(a, t, node, w, tile, v);
+  tile_weights(vocab, w, out, tile, v);
 #pragma unroll
   for (int k = 0; k < kPart; ++k) mine += v[k];
   double upto = before + (scan_add(mine) - mine);
@@ -378,150 +588,168 @@ __device__ __forceinline__ int pick(const VerifyArgs& a, const Tree& t, int node
   return tile * kTile + k * kPart + __shfl(end, k, 64);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void verify(const VerifyArgs a, int first) {
-  __shared__ double sums[kMaxTiles];
-  __shared__ double rejections[kMaxNodes];
-  __shared__ double total;
-  __shared__ int32_t parents[kMaxNodes], tokens[kMaxNodes];
-  const int s = first + blockIdx.x;
-  const Tree t = tree_of(a, s, parents, tokens);
+template <typename T, bool DRAWN>
+__global__ __launch_bounds__(64) void verify_pick(const VerifyArgs a, const Header* headers, double* tile_sums) {
+  __shared__ double sums[DRAWN ? kMaxNodes : 1];
+  __shared__ int32_t children[kMaxNodes];
+  const int s = blockIdx.x;
+  const TreeRows t = tree_rows(a, s);
   if (t.n == 0) {
-    if (threadIdx.x == 0) {
-      a.kept[s] = 0;
-      a.next[s] = -1;
-    }
+    if (threadIdx.x == 0) a.next[s] = -1;
     return;
   }
-  int32_t* path = a.path + t.row0;
-  for (int i = threadIdx.x; i < t.rows; i += kThreads) path[i] = i == 0 ? 0 : -1;
+  const Header* h = headers + s;
+  const int node = h->node, tiles = (a.vocab + kTile - 1) / kTile;
+  double* mine = tile_sums + static_cast<long>(s) * tiles;
+  const double r = a.random[t.row0];
+  Out out{children, 0};
+  int rejected = 0;
+  if constexpr (DRAWN) {
+    rejected = h->rejected;
+    for (int k = threadIdx.x; k < rejected; k += 64) sums[k] = h->sums[k];
+  } else {
+    Nodes d;
+    load_parents(a, t, d);
+    out = list_children(d, node, children, true);
+  }
   __syncthreads();
-  int node = 0, kept = 1;
-  Weights<T> w;
-  double W;
-  bool summed;  // sums and W are those of w
-  auto stand_on = [&](int i) {
-    const long row = t.row0 + i;
-    node = i;
-    w.p = static_cast<const T*>(a.p) + row * a.ld_p;
-    w.q = a.draft ? static_cast<const T*>(a.draft) + row * a.ld_draft : nullptr;
-    w.sums = rejections;
-    w.rejected = 0;
-    W = 1.0;
-    summed = false;
-  };
-  stand_on(0);
-  for (int i = next_child(t, 0, 0); i < t.n; i = next_child(t, node, i)) {
-    const int x = t.token[i];
-    const double r = a.random[t.row0 + i];
-    const bool real = x >= 0 && x < a.vocab;
-    double wx = real ? w.at(x) : 0.0;
-    double qx = 1.0;
-    if (w.q)
-      qx = real ? static_cast<double>(proper(load_one(w.q + x))) : 0.0;
-    else if (had_child(t, node, i, x))
-      wx = 0.0;
-    if (r * qx * W < wx) {
-      if (threadIdx.x == 0) path[kept] = i;
-      ++kept;
-      stand_on(i);
-    } else if (w.q) {
-      if (threadIdx.x == 0) rejections[w.rejected] = W;
-      ++w.rejected;
-      const double sum = sum_tiles(a, t, node, w, sums, &total);
-      summed = sum > 0.0;
-      if (summed)
-        W = sum;
-      else
-        --w.rejected;
-    } else {
-      W -= wx;
+  Weights<T, DRAWN> w = weights_of<T, DRAWN>(a, t, node, rejected, sums);
+  if constexpr (DRAWN) {
+    bool any = rejected == 0;
+    for (int i0 = 0; i0 < tiles && !any; i0 += 64) {
+      const int i = i0 + static_cast<int>(threadIdx.x);
+      any = __builtin_amdgcn_ballot_w64(i < tiles && mine[min(i, tiles - 1)] > 0.0) != 0;
+    }
+    if (!any) {
+      // the last rejection left nothing: the weights before it stay
+      --w.rejected;
+      for (int tile = 0; tile < tiles; ++tile) {
+        const double sum = tile_sum(a.vocab, w, out, tile);
+        if (threadIdx.x == 0) mine[tile] = sum;
+      }
+      __syncthreads();
     }
   }
-  double sum = W;
-  if (!summed) sum = sum_tiles(a, t, node, w, sums, &total);
-  if (threadIdx.x < 64) {
-    const int x = pick(a, t, node, w, sums, static_cast<double>(a.random[t.row0]) * sum);
-    if (threadIdx.x == 0) {
-      a.kept[s] = kept;
-      a.next[s] = x;
-    }
-  }
+  const int x = pick(a.vocab, w, out, mine, r);
+  if (threadIdx.x == 0) a.next[s] = x;
 }
 
 // The walk where the first maximum of each row is known: a wave to a sequence.
-__global__ __launch_bounds__(64) void verify_best(const VerifyArgs a, const int32_t* best, int first) {
-  __shared__ int32_t parents[kMaxNodes], tokens[kMaxNodes];
-  const int s = first + blockIdx.x;
-  const Tree t = tree_of(a, s, parents, tokens);
-  int node = 0, kept = t.n > 0;
-  int32_t* path = a.path + t.row0;
-  for (int i = threadIdx.x; i < t.rows; i += 64) path[i] = i == 0 ? 0 : -1;
-  int x = t.n > 0 ? best[t.row0] : -1;
-  for (int i0 = 0; i0 < t.n; i0 += 64) {
-    const int i = i0 + static_cast<int>(threadIdx.x);
-    const bool in = i < t.n;
-    const int up = in ? t.parent[i] : -1, token = in ? t.token[i] : -1;
-    const int mine = in ? best[t.row0 + i] : -1;
-    for (int from = 0; from < 64;) {
-      const uint64_t who = __builtin_amdgcn_ballot_w64(up == node && token == x && token >= 0) >> from << from;
-      if (!who) break;
-      const int k = __builtin_ctzll(who);
-      node = i0 + k;
-      x = __builtin_amdgcn_readlane(mine, k);
-      if (threadIdx.x == 0) path[kept] = node;
-      ++kept;
-      from = k + 1;
+__global__ __launch_bounds__(64) void verify_best(const VerifyArgs a, const int32_t* best) {
+  __shared__ int32_t line[kMaxNodes];
+  const int s = blockIdx.x;
+  const TreeRows t = tree_rows(a, s);
+  Nodes d;
+  load_parents(a, t, d);
+  int mine[kChunks];
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int i = 64 * c + static_cast<int>(threadIdx.x);
+    mine[c] = i < t.n ? best[t.row0 + i] : -1;
+  }
+  End e{0, 1, 0};
+  if (threadIdx.x == 0) line[0] = 0;
+  int x = of_node(mine, 0);
+  for (int i = 0; x >= 0;) {
+    int found = kMaxNodes;
+#pragma unroll
+    for (int c = kChunks - 1; c >= 0; --c) {
+      const int j = 64 * c + static_cast<int>(threadIdx.x);
+      const uint64_t who = __builtin_amdgcn_ballot_w64(d.parent[c] == e.node && j > i && d.token[c] == x);
+      if (who) found = 64 * c + __builtin_ctzll(who);
     }
+    if (found == kMaxNodes) break;
+    i = e.node = found;
+    if (threadIdx.x == 0) line[e.kept] = found;
+    ++e.kept;
+    x = of_node(mine, found);
   }
-  if (threadIdx.x == 0) {
-    a.kept[s] = kept;
-    a.next[s] = x;
+  __syncthreads();
+  store_path(a, t, s, e, line);
+  if (threadIdx.x == 0) a.next[s] = t.n > 0 ? x : -1;
+}
+
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+
+template <typename T>
+hipError_t launch_drawn(const VerifyArgs& a, hipStream_t st) {
+  Header* headers = static_cast<Header*>(a.ws);
+  double* sums = reinterpret_cast<double*>(static_cast<char*>(a.ws) + up16(sizeof(Header) * a.n_seqs));
+  // a tile to a wave, but no more workgroups than fill the chip a few times
+  const int tiles = (a.vocab + kTile - 1) / kTile, each = kSumThreads / 64;
+  const int shares = std::max(1, std::min((tiles + each - 1) / each, 2048 / a.n_seqs));
+  const dim3 grid(static_cast<unsigned>(a.n_seqs) * shares);
+  if (a.draft) {
+    hipLaunchKernelGGL(verify_walk<T>, dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a, headers);
+    hipLaunchKernelGGL((verify_sums<T, true>), grid, dim3(kSumThreads), 0, st, a, headers, sums, shares);
+    hipLaunchKernelGGL((verify_pick<T, true>), dim3(a.n_seqs), dim3(64), 0, st, a, headers, sums);
+  } else {
+    hipLaunchKernelGGL((verify_sums<T, false>), grid, dim3(kSumThreads), 0, st, a, headers, sums, shares);
+    hipLaunchKernelGGL((verify_pick<T, false>), dim3(a.n_seqs), dim3(64), 0, st, a, headers, sums);
   }
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t verify_workspace(int m, int n_seqs, int vocab) { return static_cast<size_t>(m) * sizeof(int32_t); }
+size_t verify_workspace(int m, int n_seqs, int vocab) {
+  const size_t tiles = (static_cast<size_t>(vocab) + kTile - 1) / kTile;
+  return std::max(up16(sizeof(int32_t) * static_cast<size_t>(m)),
+                  up16(sizeof(Header) * static_cast<size_t>(n_seqs)) + sizeof(double) * n_seqs * tiles);
+}
 
-hipError_t launch_probabilities(int dtype, const void* logits, long ld, const float* temperature, int m, int vocab,
-                                float* out, long ld_out, hipStream_t st) {
+namespace {
+
+template <typename T, int THREADS, int HELD>
+hipError_t launch_rows(const void* logits, long ld, const float* temperature, int m, int vocab, float* out, long ld_out,
+                       hipStream_t st) {
   for (long first = 0; first < m; first += kMaxGrid) {
     const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, m - first)));
-    if (dtype == DT_BF16)
-      hipLaunchKernelGGL(probabilities<bf16_t>, part, dim3(kProbThreads), 0, st, static_cast<const bf16_t*>(logits), ld,
-                         temperature, static_cast<int>(first), vocab, out, ld_out);
-    else
-      hipLaunchKernelGGL(probabilities<float>, part, dim3(kProbThreads), 0, st, static_cast<const float*>(logits), ld,
-                         temperature, static_cast<int>(first), vocab, out, ld_out);
+    hipLaunchKernelGGL((probabilities<T, THREADS, HELD>), part, dim3(THREADS), 0, st, static_cast<const T*>(logits), ld,
+                       temperature, static_cast<int>(first), vocab, out, ld_out);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
+template <typename T>
+hipError_t launch_probabilities_of(const void* logits, long ld, const float* temperature, int m, int vocab, float* out,
+                                   long ld_out, hipStream_t st) {
+  const long bytes = static_cast<long>(vocab) * sizeof(T);
+  // Up to 64 KB of a row many threads hold little each (7 rows of 32000 in bf16: 6.4
+  // us, 512 threads 6.9); above, two workgroups to a CU still hold 128 KB (600 rows of
+  // 65536: 56 us, 1024 threads 60, 256 threads 61).
+  const auto run = bytes <= 8l << 10    ? launch_rows<T, 256, 2>
+                   : bytes <= 64l << 10 ? launch_rows<T, 1024, 4>
+                                        : launch_rows<T, 512, 16>;
+  return run(logits, ld, temperature, m, vocab, out, ld_out, st);
+}
+
+}  // namespace
+
+hipError_t launch_probabilities(int dtype, const void* logits, long ld, const float* temperature, int m, int vocab,
+                                float* out, long ld_out, hipStream_t st) {
+  return dtype == DT_BF16 ? launch_probabilities_of<bf16_t>(logits, ld, temperature, m, vocab, out, ld_out, st)
+                          : launch_probabilities_of<float>(logits, ld, temperature, m, vocab, out, ld_out, st);
+}
+
 hipError_t launch_verify(int dtype, const VerifyArgs& a, hipStream_t st) {
   if (a.n_seqs == 0) return hipSuccess;
-  if (a.random) {
-    if (dtype == DT_BF16)
-      hipLaunchKernelGGL(verify<bf16_t>, dim3(a.n_seqs), dim3(kThreads), 0, st, a, 0);
-    else
-      hipLaunchKernelGGL(verify<float>, dim3(a.n_seqs), dim3(kThreads), 0, st, a, 0);
-    return hipGetLastError();
-  }
+  if (a.random) return dtype == DT_BF16 ? launch_drawn<bf16_t>(a, st) : launch_drawn<float>(a, st);
   int32_t* best = static_cast<int32_t*>(a.ws);
   for (long first = 0; first < a.m; first += kMaxGrid) {
     const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, a.m - first)));
     if (dtype == DT_BF16)
-      hipLaunchKernelGGL(row_best<bf16_t>, part, dim3(256), 0, st, static_cast<const bf16_t*>(a.p), a.ld_p,
+      hipLaunchKernelGGL(row_best<bf16_t>, part, dim3(kBestThreads), 0, st, static_cast<const bf16_t*>(a.p), a.ld_p,
                          static_cast<int>(first), a.vocab, best);
     else
-      hipLaunchKernelGGL(row_best<float>, part, dim3(256), 0, st, static_cast<const float*>(a.p), a.ld_p,
+      hipLaunchKernelGGL(row_best<float>, part, dim3(kBestThreads), 0, st, static_cast<const float*>(a.p), a.ld_p,
                          static_cast<int>(first), a.vocab, best);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(verify_best, dim3(a.n_seqs), dim3(64), 0, st, a, best, 0);
+  hipLaunchKernelGGL(verify_best, dim3(a.n_seqs), dim3(64), 0, st, a, best);
   return hipGetLastError();
 }
 
