@@ -88,8 +88,11 @@ struct ForkArgs {
   int32_t* writers;  // [n_pages] new rows that will write to it
   int32_t* lowest;   // [n_pages] the lowest of those
   int32_t* fresh;    // [n_pages] free pages, ascending
-  int64_t* begin;    // [n_new + 1] fresh pages given to the rows before
+  int64_t* begin;    // [n_new + 1] fresh pages given to the rows before; how many there are
+  int32_t* copied;   // [n_new] the row's last kept page is copied
   int n_new, es;
+  int width;         // fork_plan_small: slots of a sequence at most
+  Divisor by_width;
 };
 
 struct NewRow {
@@ -120,9 +123,10 @@ __device__ __forceinline__ int page_at(const PagedBatch& b, int s, int j) {
   const int page = b.table[static_cast<long>(s) * b.max_pages + j];
   return page >= 0 && page < b.n_pages ? page : -1;
 }
-// Whether the row's last kept page has to be copied: `page`.
-__device__ __forceinline__ bool needs_copy(const ForkArgs& a, const NewRow& r, int i, int page) {
-  return r.writes && page >= 0 && a.names[page] > 1 && !(a.names[page] == a.writers[page] && a.lowest[page] == i);
+// Whether row i has to copy its last kept page, which `names` rows hold and
+// `writers` rows write to, the lowest of them `lowest`.
+__device__ __forceinline__ bool needs_copy(int i, int names, int writers, int lowest) {
+  return names > 1 && !(names == writers && lowest == i);
 }
 
 __global__ __launch_bounds__(256) void fork_clear(const ForkArgs a) {
@@ -186,8 +190,10 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(const ForkArgs a) {
     int64_t mine = 0, all;
     if (i < a.n_new) {
       const NewRow r = new_row(a, i);
-      mine = r.slots - r.held;
-      if (r.writes && needs_copy(a, r, i, page_at(a.b, r.seq, r.held - 1))) ++mine;
+      const int last = r.writes ? page_at(a.b, r.seq, r.held - 1) : -1;
+      const bool copy = last >= 0 && needs_copy(i, a.names[last], a.writers[last], a.lowest[last]);
+      a.copied[i] = copy;
+      mine = r.slots - r.held + copy;
     }
     const int64_t before = sum_before(mine, waves, &all);
     if (i < a.n_new) a.begin[i] = need + before;
@@ -208,11 +214,94 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(const ForkArgs a) {
   }
 }
 
+// The same, with the clearing and the marking, where the pages' counts fit into LDS
+// and a workgroup walks all slots in a few steps.  Bound by four dependent loads and
+// the barriers between them: 144 rows of 16 sequences of 1000 to 8000 tokens in pages
+// of 64 take 6.7 us, the three kernels above 1.7, 3.5 and 5.2 and two more launches.
+constexpr int kSmallPages = 8192;
+constexpr int kSmallSlots = 32 * kPlanThreads;
+
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_small(const ForkArgs a) {
+  constexpr int PER = kSmallPages / kPlanThreads;
+  __shared__ int names[kSmallPages], writers[kSmallPages], lowest[kSmallPages];
+  __shared__ unsigned char used[kSmallPages];
+  __shared__ int row_seq[kPlanThreads], row_held[kPlanThreads], old_slots[kPlanThreads], heirs[kPlanThreads];
+  __shared__ int64_t waves[kPlanThreads / 64];
+  const int tid = threadIdx.x;
+  NewRow r{};
+  if (tid < a.n_new) r = new_row(a, tid);
+  const int slots = tid < a.b.n_seqs ? slots_of(a.b, old_length(a.b, tid)) : 0;
+  const int last = tid < a.n_new && r.writes ? page_at(a.b, r.seq, r.held - 1) : -1;
+  row_seq[tid] = r.seq;
+  row_held[tid] = r.held;
+  old_slots[tid] = slots;
+  heirs[tid] = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int p = tid + k * kPlanThreads;
+    names[p] = writers[p] = 0;
+    lowest[p] = kPlanThreads;
+    used[p] = 0;
+  }
+  __syncthreads();
+  // rows that keep all of their sequence hold what it holds
+  if (!a.keep && r.held > 0) atomicAdd(heirs + r.seq, 1);
+  __syncthreads();
+  const int total = (a.b.n_seqs + (a.keep ? a.n_new : 0)) * a.width;
+  for (int k0 = tid; k0 < total; k0 += 4 * kPlanThreads) {
+    int page[4], count[4];  // rows that name the page; -1: the sequence itself
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = min(k0 + u * kPlanThreads, total - 1);
+      const int w = div_by(k, a.by_width.magic, a.by_width.shift), j = k - w * a.width;
+      const bool old = w < a.b.n_seqs;
+      const int i = old ? w : w - a.b.n_seqs;
+      const bool in = k0 + u * kPlanThreads < total && j < (old ? old_slots[i] : row_held[i]);
+      page[u] = page_at(a.b, old ? i : row_seq[i], min(j, a.b.max_pages - 1));
+      if (!in) page[u] = -1;
+      count[u] = old ? (a.keep ? -1 : -1 - heirs[i]) : 1;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (page[u] < 0) continue;
+      if (count[u] < 0) used[page[u]] = 1;
+      const int rows = count[u] < 0 ? -1 - count[u] : count[u];
+      if (rows > 0) atomicAdd(names + page[u], rows);
+    }
+  }
+  if (last >= 0) {
+    atomicAdd(writers + last, 1);
+    atomicMin(lowest + last, tid);
+  }
+  __syncthreads();
+  const bool copy = last >= 0 && needs_copy(tid, names[last], writers[last], lowest[last]);
+  int64_t need, have;
+  const int64_t begin = sum_before(tid < a.n_new ? r.slots - r.held + copy : 0, waves, &need);
+  if (tid < a.n_new) {
+    a.begin[tid] = begin;
+    a.copied[tid] = copy;
+  }
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) mine += PER * tid + k < a.b.n_pages && !used[PER * tid + k];
+  int64_t rank = sum_before(mine, waves, &have);
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    if (PER * tid + k < a.b.n_pages && !used[PER * tid + k]) {
+      if (rank < need) a.fresh[rank] = PER * tid + k;
+      ++rank;
+    }
+  if (tid == 0) {
+    a.begin[a.n_new] = have;
+    *a.missing = static_cast<int32_t>(min(max(need - have, int64_t{0}), int64_t{0x7FFFFFFF}));
+  }
+}
+
 __global__ __launch_bounds__(256) void fork_rows(const ForkArgs a, int shares) {
   const int i = blockIdx.x / shares, share = blockIdx.x % shares;
   const NewRow r = new_row(a, i);
-  const int last = r.writes ? page_at(a.b, r.seq, r.held - 1) : -1;
-  const bool copy = needs_copy(a, r, i, last);
+  const bool copy = a.copied[i] != 0;
+  const int last = copy ? page_at(a.b, r.seq, r.held - 1) : -1;
   const int own = r.held - copy;  // slots from here on are fresh
   const int64_t begin = a.begin[i], have = a.begin[a.n_new];
   auto fresh = [&](int j) { return begin + j - own < have ? a.fresh[begin + j - own] : -1; };
@@ -222,7 +311,7 @@ __global__ __launch_bounds__(256) void fork_rows(const ForkArgs a, int shares) {
       row[j] = j < own ? page_at(a.b, r.seq, j) : (j < r.slots ? fresh(j) : -1);
     if (threadIdx.x == 0) a.kv_out[i] = r.length;
   }
-  if (!copy) return;
+  if (last < 0) return;
   const int to = fresh(own);
   if (to < 0) return;
   const int rows = r.keep & ((1 << a.b.page_shift) - 1);
@@ -257,7 +346,8 @@ hipError_t launch_paged_keep(int dtype, const PagedBatch& b, int m, const int32_
 }
 
 size_t paged_fork_workspace(const PagedBatch& b, int n_new) {
-  return 5 * up16(sizeof(int32_t) * static_cast<size_t>(b.n_pages)) + sizeof(int64_t) * (static_cast<size_t>(n_new) + 1);
+  return 5 * up16(sizeof(int32_t) * static_cast<size_t>(b.n_pages)) +
+         up16(sizeof(int64_t) * (static_cast<size_t>(n_new) + 1)) + sizeof(int32_t) * static_cast<size_t>(n_new);
 }
 
 hipError_t launch_paged_fork(int dtype, const PagedBatch& b, int n_new, const int32_t* source, const int32_t* keep,
@@ -277,11 +367,21 @@ hipError_t launch_paged_fork(int dtype, const PagedBatch& b, int n_new, const in
     at += up16(sizeof(int32_t) * static_cast<size_t>(b.n_pages));
   }
   a.begin = reinterpret_cast<int64_t*>(at);
+  a.copied = reinterpret_cast<int32_t*>(at + up16(sizeof(int64_t) * (static_cast<size_t>(n_new) + 1)));
   a.n_new = n_new;
   a.es = dtype == DT_BF16 ? 2 : 4;
-  hipLaunchKernelGGL(fork_clear, dim3((b.n_pages + 255u) / 256u), dim3(256), 0, st, a);
-  if (b.n_seqs + n_new > 0) hipLaunchKernelGGL(fork_mark, dim3(b.n_seqs + n_new), dim3(256), 0, st, a);
-  hipLaunchKernelGGL(fork_plan, dim3(1), dim3(kPlanThreads), 0, st, a);
+  a.width = (b.max_kv + (1 << b.page_shift) - 1) >> b.page_shift;
+  a.by_width = make_divisor(a.width);
+  if (b.n_pages <= kSmallPages && b.n_seqs <= kPlanThreads && n_new <= kPlanThreads &&
+      static_cast<long>(b.n_seqs + (keep ? n_new : 0)) * a.width <= kSmallSlots) {
+    hipLaunchKernelGGL(fork_plan_small, dim3(1), dim3(kPlanThreads), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(fork_clear, dim3((b.n_pages + 255u) / 256u), dim3(256), 0, st, a);
+    if (b.n_seqs + n_new > 0) hipLaunchKernelGGL(fork_mark, dim3(b.n_seqs + n_new), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(fork_plan, dim3(1), dim3(kPlanThreads), 0, st, a);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   if (n_new > 0) {
     const int shares = 8;
     hipLaunchKernelGGL(fork_rows, dim3(static_cast<unsigned>(n_new) * shares), dim3(256), 0, st, a, shares);
