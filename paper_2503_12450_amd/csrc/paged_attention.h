@@ -208,8 +208,8 @@ __device__ __forceinline__ Row make_row(const AttnArgs& a, const Tile& t, int hk
 // words of LDS for it alone that its wave reads; its depth bounds what it sees of the
 // past.  The parents of the tree's nodes lie in the wave's registers, 64 to a word's
 // register, and every lane walks up from its node by lane permutes: as many steps
-// as the deepest has ancestors (at most kMaxTree: a parent comes before its child),
-// twice if there is a window, which needs the depth first.  All lanes take part.
+// as the deepest has ancestors (at most kMaxTree: a parent comes before its child).
+// All lanes take part.
 __device__ __forceinline__ void add_nodes(const AttnArgs& a, const Tile& t, int i, uint64_t* nodes, Row& row) {
   const int lane = threadIdx.x & 63;
   const int node = div_by(t.r0 + min(i, t.n - 1), a.by_group.magic, a.by_group.shift);
@@ -233,19 +233,26 @@ __device__ __forceinline__ void add_nodes(const AttnArgs& a, const Tile& t, int 
       }
     return p;
   };
-  int depth = 0;
-  if (a.window) {
-    for (int k = above(node); __builtin_amdgcn_ballot_w64(k >= 0) != 0; k = above(k)) depth += k >= 0;
-    row.lo = row_lo(a, t.sp.first + depth);
-  }
   uint64_t set[kTreeWords] = {};
-  int back = 0;  // steps up from the row's own node
-  for (int k = node; __builtin_amdgcn_ballot_w64(k >= 0) != 0; k = above(k), ++back) {
+  int depth = -1;
+  for (int k = node; __builtin_amdgcn_ballot_w64(k >= 0) != 0; k = above(k)) {
     const int token = t.sp.first + k;
-    const bool near = !a.window || back < a.window || t.sp.first + depth - back < a.sinks;
-    const uint64_t bit = k >= 0 && near && token >= 0 && token < t.sp.len ? uint64_t{1} << (k & 63) : 0;
+    const uint64_t bit = k >= 0 && token >= 0 && token < t.sp.len ? uint64_t{1} << (k & 63) : 0;
 #pragma unroll
     for (int w = 0; w < kTreeWords; ++w) set[w] |= k >> 6 == w ? bit : 0;
+    depth += k >= 0;
+  }
+  if (a.window) {
+    row.lo = row_lo(a, t.sp.first + depth);
+    // where a tree is deeper than the window, again without the ancestors outside it
+    if (__builtin_amdgcn_ballot_w64(depth >= a.window) != 0) {
+      int back = 0;  // steps up from the row's own node
+      for (int k = node; __builtin_amdgcn_ballot_w64(k >= 0) != 0; k = above(k), ++back) {
+        const bool far = k >= 0 && back >= a.window && t.sp.first + depth - back >= a.sinks;
+#pragma unroll
+        for (int w = 0; w < kTreeWords; ++w) set[w] &= far && k >> 6 == w ? ~(uint64_t{1} << (k & 63)) : ~uint64_t{0};
+      }
+    }
   }
 #pragma unroll
   for (int w = 0; w < kTreeWords; ++w) nodes[w] = set[w];
@@ -621,6 +628,10 @@ __device__ __forceinline__ void work_item(const AttnArgs& a, int& tile, int& hk,
   part = r / a.tiles;
   tile = r - part * a.tiles;
 }
+// Parts of a tile of `count` blocks.
+__device__ __forceinline__ int tile_parts(const AttnArgs& a, int count) {
+  return max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
+}
 __device__ __forceinline__ void part_range(const AttnArgs& a, int part, int count, int& from, int& to) {
   from = part * a.part_blocks;
   to = part == a.parts - 1 ? count : min(count, from + a.part_blocks);
@@ -797,7 +808,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   part_range(a, part, blocks.count, from, to);
   if (from >= to && from > 0) return;
   Row row = make_row(a, tile, hk, c);
-  if constexpr (kTree) add_nodes(a, tile, c, nodes[wave * 32 + c], row);
   u32x4_t qf[G::DS];
   load_q<DH>(a, row, hg, qf);
   const Reach reach = rows_reach(a, tile, 0, tile.n);
@@ -825,6 +835,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
   };
   RowState<DH> st;
   if (from + wave < to) load_block(from + wave);
+  if constexpr (kTree) add_nodes(a, tile, c, nodes[wave * 32 + c], row);  // while they are on their way
   for (int i = from + wave; i < to; i += kWaves) {
     const uint64_t alive = alive_next;
     const int key0 = blocks.at(i) * KB;
@@ -933,7 +944,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     Row row = make_row(a, tile, hk, 16 * qt + c);
-    if constexpr (kTree) add_nodes(a, tile, 16 * qt + c, nodes[wave][16 * qt + c], row);
     key_hi[qt] = row.hi;
     key_lo[qt] = row.lo;
     const float* qr = static_cast<const float*>(a.q) + row.q_at + g * DL;
@@ -982,6 +992,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
     load_keys();
     load_values();
   }
+  if constexpr (kTree)
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      Row row = make_row(a, tile, hk, 16 * qt + c);
+      add_nodes(a, tile, 16 * qt + c, nodes[wave][16 * qt + c], row);
+      key_lo[qt] = row.lo;
+    }
   for (int i = from + wave; i < to; i += kWaves) {
     const int key0 = blocks.at(i) * KB;
     const bool alive = alive_next, more = i + kWaves < to;
@@ -1154,7 +1171,7 @@ __global__ __launch_bounds__(256) void attn_join(const AttnArgs a, int kb, int r
   const Tile t = find_tile(a, w / shares);
   if (share * rows >= t.n) return;
   const int count = tile_blocks(a, t, kb).count;
-  const int parts = max(1, min(a.parts, (count + a.part_blocks - 1) / a.part_blocks));
+  const int parts = tile_parts(a, count);
   if (kTree && parts == 1) return;
   const int octet = threadIdx.x >> 3, subs = 32 / rows;  // octets of a row
   const int sub = octet % subs;
@@ -1267,6 +1284,10 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   if (kTree && p.kind == MANY)
     parts = std::min({std::max<long>(512 / items, (blocks + 39) / 40), static_cast<long>(blocks) / 8,
                       std::max(4096 / items, 1l)});
+  // Trees, 32 rows to a tile: the join costs more than dividing a few blocks saves (6
+  // trees of 20 nodes, 12 heads of 64: 600 keys 10 us, in two parts 14; 1500 keys 15, in
+  // four 17.5; 16 of 6, 8 heads of 128 on 2, 1500 keys: 24, in four 20).
+  if (kTree && p.kind == FEW && blocks < (b.d_head <= 64 ? 48 : 24)) parts = 1;
   parts = std::max(parts, 1l);
   const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
   parts = std::max(1l, std::min<long>(parts, static_cast<long>(ws_bytes / per_part)));
