@@ -570,6 +570,14 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
 # drafted tokens
 # --------------------------------------------------------------------------
 
+def _ints(device, i32, n: int, **tensors) -> None:
+    """Each of the tensors (None: not given) is a dense vector of n int32 on
+    `device`."""
+    for name, t in tensors.items():
+        if t is not None and not (t.dtype is i32 and t.shape == (n,) and t.device == device and t.is_contiguous()):
+            _dense(name, t, i32, (n,), device)
+
+
 def _workspace(workspace, device):
     """(pointer, bytes) of a workspace tensor of any type, or of None."""
     if workspace is None:
@@ -611,7 +619,7 @@ def k_paged_tree_attention(batch: PagedBatch, q, parent, out, window: int = 0, s
     heads_out, ldo = _rows("out", out, dtype, m, dh, dev)
     if heads_out != heads:
         _refuse("out and q differ in width")
-    _dense("parent", parent, _torch().int32, (m,), dev)
+    _ints(dev, batch.kv_len.dtype, m, parent=parent)
     ws_ptr, ws_bytes = _workspace(workspace, dev)
     if (m | heads | window | sinks) >> 31:
         _int32("rows, heads, window, sinks", m, heads, window, sinks)
@@ -663,12 +671,9 @@ def k_draft_verify(q_start, p, parent, tokens, path, kept, next_token, random=No
     ldd = _vocab_rows("draft", draft, dtype, shape, dev) if draft is not None else 0
     m, vocab = shape
     n_seqs, i32 = q_start.shape[0] - 1, torch.int32
-    _dense("q_start", q_start, i32, (n_seqs + 1,), dev)
-    _dense("parent", parent, i32, (m,), dev)
-    _dense("tokens", tokens, i32, (m,), dev)
-    _dense("path", path, i32, (m,), dev)
-    _dense("kept", kept, i32, (n_seqs,), dev)
-    _dense("next_token", next_token, i32, (n_seqs,), dev)
+    _ints(dev, i32, n_seqs + 1, q_start=q_start)
+    _ints(dev, i32, m, parent=parent, tokens=tokens, path=path)
+    _ints(dev, i32, n_seqs, kept=kept, next_token=next_token)
     if random is not None:
         _dense("random", random, torch.float32, (m,), dev)
     ws_ptr, ws_bytes = _workspace(workspace, dev)
@@ -684,11 +689,10 @@ def k_paged_keep(batch: PagedBatch, path, kept, kv_len_out, stream=None) -> None
     """The kept nodes' keys and values (path [m], kept [seqs] as k_draft_verify
     leaves them) moved together in the batch's pages; kv_len_out [seqs]: the
     lengths that remain."""
-    dev, i32, n = batch.device, _torch().int32, batch.kv_len.shape[0]
+    dev, i32, n = batch.device, batch.kv_len.dtype, batch.c.n_seqs
     m = path.shape[0] if len(path.shape) == 1 else -1
-    _dense("path", path, i32, (None,), dev)
-    _dense("kept", kept, i32, (n,), dev)
-    _dense("kv_len_out", kv_len_out, i32, (n,), dev)
+    _ints(dev, i32, m, path=path)
+    _ints(dev, i32, n, kept=kept, kv_len_out=kv_len_out)
     if m >> 31:
         _int32("rows", m)
     _check(load().mar_k_paged_keep(batch.code, batch.ref, m, path.data_ptr(), kept.data_ptr(), kv_len_out.data_ptr(),
@@ -710,15 +714,11 @@ def k_paged_fork(batch: PagedBatch, source, table_out, kv_len_out, missing, keep
     """A new table: row i continues sequence source[i] with its first keep[i]
     tokens (None: all) and room for add[i] more (None: none).  table_out [n,
     max_pages], kv_len_out [n], missing [1]; source, keep, add [n]; all int32."""
-    dev, i32 = batch.device, _torch().int32
-    _dense("source", source, i32, (None,), dev)
-    n = source.shape[0]
-    _dense("table_out", table_out, i32, (n, batch.table.shape[1]), dev)
-    _dense("kv_len_out", kv_len_out, i32, (n,), dev)
-    _dense("missing", missing, i32, (1,), dev)
-    for name, t in (("keep", keep), ("add", add)):
-        if t is not None:
-            _dense(name, t, i32, (n,), dev)
+    dev, i32 = batch.device, batch.kv_len.dtype
+    n = source.shape[0] if len(source.shape) == 1 else -1
+    _ints(dev, i32, n, source=source, kv_len_out=kv_len_out, keep=keep, add=add)
+    _dense("table_out", table_out, i32, (n, batch.c.max_pages), dev)
+    _ints(dev, i32, 1, missing=missing)
     ws_ptr, ws_bytes = _workspace(workspace, dev)
     if n >> 31:
         _int32("rows", n)

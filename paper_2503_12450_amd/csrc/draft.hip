@@ -214,9 +214,13 @@ __global__ __launch_bounds__(kBestThreads) void row_best(const T* p, long ld, in
 //                 each workgroup repeats the walk, which costs less than a launch
 //   verify_pick   the tile that the random number falls into, and the token in it,
 //                 a wave to a sequence
-// Bound by the chain of dependent loads of each: TIMES.
+// Bound by the three or four dependent loads of each (48 chains of 5 to 9, 65536 tokens
+// in fp32: 5.5, 5.2 and 4.8 us, of which reading p and q once would take 4.9; 32 trees
+// of 16 to 64, 100003 tokens: 6.5 and 4.5).
+//   verify_whole  all of it, a workgroup to a sequence: for few tokens, and for as many
+//                 sequences as fill the chip
 // ---------------------------------------------------------------------------
-constexpr int kWalkThreads = 1024;
+constexpr int kWalkThreads = 512;
 constexpr int kSumThreads = 256;
 constexpr int kTile = 1024;  // tokens of which a wave sums the weights
 constexpr int kPart = kTile / 64;
@@ -242,10 +246,12 @@ __device__ __forceinline__ TreeRows tree_rows(const VerifyArgs& a, int s) {
 // Node 64 c + lane in element c: its parent (-1: none), token, random number, and p
 // and q of the token in the parent's rows.
 struct Nodes {
+  int n;
   int parent[kChunks], token[kChunks];
   float r[kChunks], p[kChunks], q[kChunks];
 };
 __device__ __forceinline__ void load_parents(const VerifyArgs& a, const TreeRows& t, Nodes& d) {
+  d.n = t.n;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     d.parent[c] = d.token[c] = -1;
@@ -273,7 +279,8 @@ __device__ __forceinline__ void load_nodes(const VerifyArgs& a, const TreeRows& 
   }
 }
 __device__ __forceinline__ int of_node(const int (&v)[kChunks], int i) {
-  int x = __builtin_amdgcn_readlane(v[0], i & 63);
+  if (i < 64) return __builtin_amdgcn_readlane(v[0], i);
+  int x = 0;
 #pragma unroll
   for (int c = 1; c < kChunks; ++c)
     if (i >> 6 == c) x = __builtin_amdgcn_readlane(v[c], i & 63);
@@ -290,6 +297,7 @@ __device__ __forceinline__ int next_child(const Nodes& d, int node, int after) {
   int found = kMaxNodes;
 #pragma unroll
   for (int c = kChunks - 1; c >= 0; --c) {
+    if (64 * c >= d.n) continue;
     const int i = 64 * c + static_cast<int>(threadIdx.x & 63);
     const uint64_t who = __builtin_amdgcn_ballot_w64(d.parent[c] == node && i > after);
     if (who) found = 64 * c + __builtin_ctzll(who);
@@ -301,6 +309,7 @@ __device__ __forceinline__ bool had_child(const Nodes& d, int node, int i, int x
   uint64_t who = 0;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
+    if (64 * c >= d.n) continue;
     const int j = 64 * c + static_cast<int>(threadIdx.x & 63);
     who |= __builtin_amdgcn_ballot_w64(d.parent[c] == node && j < i && d.token[c] == x);
   }
@@ -344,6 +353,7 @@ __device__ __forceinline__ Out list_children(const Nodes& d, int node, int32_t* 
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
+    if (64 * c >= d.n) continue;
     const bool mine = d.parent[c] == node;
     const uint64_t who = __builtin_amdgcn_ballot_w64(mine);
     if (mine && write) token[o.n + __builtin_popcountll(who & ((uint64_t{1} << lane) - 1))] = d.token[c];
@@ -352,46 +362,68 @@ __device__ __forceinline__ Out list_children(const Nodes& d, int node, int32_t* 
   return o;
 }
 
-// The weights of a tile's tokens, 16 to a lane, in order.
+// A tile's values, 16 tokens to a lane, in order.
+struct Values {
+  float p[kPart], q[kPart];
+};
 template <typename T, bool DRAWN>
-__device__ __forceinline__ void tile_weights(int vocab, const Weights<T, DRAWN>& w, const Out& out, int tile,
-                                             double (&v)[kPart]) {
+__device__ __forceinline__ Values load_tile(int vocab, const Weights<T, DRAWN>& w, int tile) {
   constexpr int N = kPer<T>;
-  const int lane = threadIdx.x & 63, i0 = tile * kTile + lane * kPart;
-  float pv[kPart], qv[kPart] = {};
+  const int i0 = tile * kTile + static_cast<int>(threadIdx.x & 63) * kPart;
+  Values x{};
   if (i0 + kPart <= vocab) {
 #pragma unroll
     for (int k = 0; k < kPart; k += N) {
-      unpack16(load_any(w.p + i0 + k), pv + k, static_cast<const T*>(nullptr));
-      if (DRAWN) unpack16(load_any(w.q + i0 + k), qv + k, static_cast<const T*>(nullptr));
+      unpack16(load_any(w.p + i0 + k), x.p + k, static_cast<const T*>(nullptr));
+      if (DRAWN) unpack16(load_any(w.q + i0 + k), x.q + k, static_cast<const T*>(nullptr));
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < kPart; ++k) {
-      pv[k] = i0 + k < vocab ? load_one(w.p + i0 + k) : 0.f;
-      if (DRAWN) qv[k] = i0 + k < vocab ? load_one(w.q + i0 + k) : 0.f;
+    for (int k = 0; k < kPart; ++k) {  // none behind a branch: they are on their way together
+      x.p[k] = load_one(w.p + min(i0 + k, vocab - 1));
+      if (DRAWN) x.q[k] = load_one(w.q + min(i0 + k, vocab - 1));
     }
-  }
 #pragma unroll
-  for (int k = 0; k < kPart; ++k) v[k] = w.of(proper(pv[k]), proper(qv[k]));
+    for (int k = 0; k < kPart; ++k) x.p[k] = i0 + k < vocab ? x.p[k] : 0.f;
+  }
+  return x;
+}
+// Their weights.
+template <typename T, bool DRAWN>
+__device__ __forceinline__ void tile_weights(const Values& x, const Weights<T, DRAWN>& w, const Out& out, int tile,
+                                             double (&v)[kPart]) {
+  const int lane = threadIdx.x & 63, i0 = tile * kTile + lane * kPart;
+#pragma unroll
+  for (int k = 0; k < kPart; ++k) v[k] = w.of(proper(x.p[k]), proper(x.q[k]));
   if (DRAWN) return;
   for (int j0 = 0; j0 < out.n; j0 += 64) {
-    const int x = j0 + lane < out.n ? out.token[j0 + lane] : -1;
-    for (uint64_t who = __builtin_amdgcn_ballot_w64(x >= 0 && x / kTile == tile); who; who &= who - 1) {
-      const int at = __builtin_amdgcn_readlane(x, __builtin_ctzll(who)) - i0;
+    const int t = j0 + lane < out.n ? out.token[j0 + lane] : -1;
+    for (uint64_t who = __builtin_amdgcn_ballot_w64(t >= 0 && t / kTile == tile); who; who &= who - 1) {
+      const int at = __builtin_amdgcn_readlane(t, __builtin_ctzll(who)) - i0;
 #pragma unroll
       for (int k = 0; k < kPart; ++k)
         if (k == at) v[k] = 0.0;
     }
   }
 }
-template <typename T, bool DRAWN>
-__device__ __forceinline__ double tile_sum(int vocab, const Weights<T, DRAWN>& w, const Out& out, int tile) {
-  double v[kPart], sum = 0.0;
-  tile_weights(vocab, w, out, tile, v);
+// Sums of the tiles from, from + step, ... by one wave, the next tile's values on
+// their way meanwhile: take(tile, sum).
+template <typename T, bool DRAWN, typename Take>
+__device__ __forceinline__ void sum_tiles(int vocab, const Weights<T, DRAWN>& w, const Out& out, int from, int step,
+                                          Take&& take) {
+  const int tiles = (vocab + kTile - 1) / kTile;
+  if (from >= tiles) return;
+  Values x = load_tile(vocab, w, from);
+  for (int tile = from; tile < tiles; tile += step) {
+    Values next;
+    if (tile + step < tiles) next = load_tile(vocab, w, tile + step);
+    double v[kPart], sum = 0.0;
+    tile_weights(x, w, out, tile, v);
 #pragma unroll
-  for (int k = 0; k < kPart; ++k) sum += v[k];
-  return wave_sum(sum);
+    for (int k = 0; k < kPart; ++k) sum += v[k];
+    take(tile, wave_sum(sum));
+    if (tile + step < tiles) x = next;
+  }
 }
 
 // How a walk ended.
@@ -461,11 +493,10 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk(const VerifyArgs a, 
   const TreeRows t = tree_rows(a, s);
   Nodes d;
   load_nodes<T, true>(a, t, d);
-  const int tiles = (a.vocab + kTile - 1) / kTile;
   const End e = walk<T, true>(a, t, d, line, threadIdx.x == 0, sums, [&](const Weights<T, true>& w) {
     __syncthreads();  // W of the rejection is there, the sums before are read
     double sum = 0.0;
-    for (int tile = wave; tile < tiles; tile += kWalkThreads / 64) sum += tile_sum(a.vocab, w, Out{nullptr, 0}, tile);
+    sum_tiles(a.vocab, w, Out{nullptr, 0}, wave, kWalkThreads / 64, [&](int, double x) { sum += x; });
     if ((threadIdx.x & 63) == 0) part[wave] = sum;
     __syncthreads();
     sum = 0.0;
@@ -496,8 +527,10 @@ __global__ __launch_bounds__(kSumThreads) void verify_sums(const VerifyArgs a, H
     if (t.n == 0) return;
     node = h->node;
     rejected = h->rejected;
-    for (int k = threadIdx.x; k < rejected; k += kSumThreads) sums[k] = h->sums[k];
-    __syncthreads();
+    if (rejected > 1) {  // the first is 1
+      for (int k = threadIdx.x; k < rejected; k += kSumThreads) sums[k] = h->sums[k];
+      __syncthreads();
+    }
   } else {
     Nodes d;
     load_nodes<T, false>(a, t, d);
@@ -513,10 +546,17 @@ __global__ __launch_bounds__(kSumThreads) void verify_sums(const VerifyArgs a, H
   }
   const Weights<T, DRAWN> w = weights_of<T, DRAWN>(a, t, node, rejected, sums);
   const int tiles = (a.vocab + kTile - 1) / kTile;
-  for (int tile = share * (kSumThreads / 64) + (threadIdx.x >> 6); tile < tiles; tile += shares * (kSumThreads / 64)) {
-    const double sum = tile_sum(a.vocab, w, out, tile);
+  constexpr int waves = kSumThreads / 64;
+  sum_tiles(a.vocab, w, out, share * waves + (threadIdx.x >> 6), shares * waves, [&](int tile, double sum) {
     if ((threadIdx.x & 63) == 0) tile_sums[static_cast<long>(s) * tiles + tile] = sum;
-  }
+  });
+}
+
+// The lane's share of the tiles' sums.
+__device__ __forceinline__ double lane_total(const double* tile_sums, int tiles) {
+  double total = 0.0;
+  for (int i = threadIdx.x & 63; i < tiles; i += 64) total += tile_sums[i];
+  return total;
 }
 
 // v summed over the lanes up to and with this one.
@@ -531,13 +571,12 @@ __device__ __forceinline__ double scan_add(double v) {
 }
 
 // The first token at which the summed weights pass r times their sum, given the tiles'
-// sums; the last one with a weight if none does.  -1 if none has any.
+// sums (total: the lanes' shares of them); the last one with a weight if none does.  -1
+// if none has any.
 template <typename T, bool DRAWN>
 __device__ __forceinline__ int pick(int vocab, const Weights<T, DRAWN>& w, const Out& out, const double* tile_sums,
-                                    double r) {
+                                    double total, double r) {
   const int tiles = (vocab + kTile - 1) / kTile, lane = threadIdx.x & 63;
-  double total = 0.0;
-  for (int i = lane; i < tiles; i += 64) total += tile_sums[i];
   const double goal = r * wave_sum(total);
   double before = 0.0, last_before = 0.0;
   int tile = -1, last = -1;
@@ -565,7 +604,7 @@ __device__ __forceinline__ int pick(int vocab, const Weights<T, DRAWN>& w, const
     before = last_before;
   }
   double v[kPart], mine = 0.0;
-  tile_weights(vocab, w, out, tile, v);
+  tile_weights(load_tile(vocab, w, tile), w, out, tile, v);
 #pragma unroll
   for (int k = 0; k < kPart; ++k) mine += v[k];
   double upto = before + (scan_add(mine) - mine);
@@ -592,21 +631,23 @@ template <typename T, bool DRAWN>
 __global__ __launch_bounds__(64) void verify_pick(const VerifyArgs a, const Header* headers, double* tile_sums) {
   __shared__ double sums[DRAWN ? kMaxNodes : 1];
   __shared__ int32_t children[kMaxNodes];
-  const int s = blockIdx.x;
+  const int s = blockIdx.x, tiles = (a.vocab + kTile - 1) / kTile;
+  // loads that wait for none (a sequence without rows left nothing to read, but room)
+  const Header* h = headers + s;
+  double* mine = tile_sums + static_cast<long>(s) * tiles;
+  const int node = h->node;
+  int rejected = DRAWN ? h->rejected : 0;
+  double total = lane_total(mine, tiles);
   const TreeRows t = tree_rows(a, s);
   if (t.n == 0) {
     if (threadIdx.x == 0) a.next[s] = -1;
     return;
   }
-  const Header* h = headers + s;
-  const int node = h->node, tiles = (a.vocab + kTile - 1) / kTile;
-  double* mine = tile_sums + static_cast<long>(s) * tiles;
   const double r = a.random[t.row0];
   Out out{children, 0};
-  int rejected = 0;
   if constexpr (DRAWN) {
-    rejected = h->rejected;
-    for (int k = threadIdx.x; k < rejected; k += 64) sums[k] = h->sums[k];
+    if (rejected > 1)
+      for (int k = threadIdx.x; k < rejected; k += 64) sums[k] = h->sums[k];
   } else {
     Nodes d;
     load_parents(a, t, d);
@@ -615,23 +656,68 @@ __global__ __launch_bounds__(64) void verify_pick(const VerifyArgs a, const Head
   __syncthreads();
   Weights<T, DRAWN> w = weights_of<T, DRAWN>(a, t, node, rejected, sums);
   if constexpr (DRAWN) {
-    bool any = rejected == 0;
-    for (int i0 = 0; i0 < tiles && !any; i0 += 64) {
-      const int i = i0 + static_cast<int>(threadIdx.x);
-      any = __builtin_amdgcn_ballot_w64(i < tiles && mine[min(i, tiles - 1)] > 0.0) != 0;
-    }
+    const bool any = rejected == 0 || __builtin_amdgcn_ballot_w64(total > 0.0) != 0;
     if (!any) {
       // the last rejection left nothing: the weights before it stay
       --w.rejected;
-      for (int tile = 0; tile < tiles; ++tile) {
-        const double sum = tile_sum(a.vocab, w, out, tile);
+      sum_tiles(a.vocab, w, out, 0, 1, [&](int tile, double sum) {
         if (threadIdx.x == 0) mine[tile] = sum;
-      }
+      });
       __syncthreads();
+      total = lane_total(mine, tiles);
     }
   }
-  const int x = pick(a.vocab, w, out, mine, r);
+  const int x = pick(a.vocab, w, out, mine, total, r);
   if (threadIdx.x == 0) a.next[s] = x;
+}
+
+// All of it by one workgroup to a sequence.
+template <typename T, bool DRAWN>
+__global__ __launch_bounds__(kWalkThreads) void verify_whole(const VerifyArgs a) {
+  constexpr int WAVES = kWalkThreads / 64;
+  __shared__ double tile_sums[kMaxVocab / kTile], sums[DRAWN ? kMaxNodes : 1], part[WAVES];
+  __shared__ int32_t line[kMaxNodes], children[kMaxNodes];
+  const int s = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const TreeRows t = tree_rows(a, s);
+  if (t.n == 0) {
+    if (threadIdx.x == 0) {
+      a.kept[s] = 0;
+      a.next[s] = -1;
+    }
+    return;
+  }
+  const double r = a.random[t.row0];
+  Nodes d;
+  load_nodes<T, DRAWN>(a, t, d);
+  // the tiles' sums to LDS, their total (of the waves' in order) to all
+  auto sum_all = [&](const Weights<T, DRAWN>& w, const Out& out) {
+    __syncthreads();  // what w and out read in LDS is there, the sums before are read
+    double sum = 0.0;
+    sum_tiles(a.vocab, w, out, wave, WAVES, [&](int tile, double x) {
+      sum += x;
+      if (lane == 0) tile_sums[tile] = x;
+    });
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int k = 0; k < WAVES; ++k) sum += part[k];
+    return sum;
+  };
+  const End e = walk<T, DRAWN>(a, t, d, line, threadIdx.x == 0, sums,
+                               [&](const Weights<T, DRAWN>& w) { return sum_all(w, Out{nullptr, 0}); });
+  Out out{children, 0};
+  if (!DRAWN) out = list_children(d, e.node, children, wave == 0);
+  Weights<T, DRAWN> w = weights_of<T, DRAWN>(a, t, e.node, e.rejected, sums);
+  if (!(sum_all(w, out) > 0.0) && DRAWN && w.rejected > 0) {
+    // the last rejection left nothing: the weights before it stay
+    --w.rejected;
+    sum_all(w, out);
+  }
+  store_path(a, t, s, e, line);
+  if (wave == 0) {
+    const int x = pick(a.vocab, w, out, tile_sums, lane_total(tile_sums, (a.vocab + kTile - 1) / kTile), r);
+    if (lane == 0) a.next[s] = x;
+  }
 }
 
 // The walk where the first maximum of each row is known: a wave to a sequence.
@@ -654,6 +740,7 @@ __global__ __launch_bounds__(64) void verify_best(const VerifyArgs a, const int3
     int found = kMaxNodes;
 #pragma unroll
     for (int c = kChunks - 1; c >= 0; --c) {
+      if (64 * c >= d.n) continue;
       const int j = 64 * c + static_cast<int>(threadIdx.x);
       const uint64_t who = __builtin_amdgcn_ballot_w64(d.parent[c] == e.node && j > i && d.token[c] == x);
       if (who) found = 64 * c + __builtin_ctzll(who);
@@ -677,6 +764,16 @@ hipError_t launch_drawn(const VerifyArgs& a, hipStream_t st) {
   double* sums = reinterpret_cast<double*>(static_cast<char*>(a.ws) + up16(sizeof(Header) * a.n_seqs));
   // a tile to a wave, but no more workgroups than fill the chip a few times
   const int tiles = (a.vocab + kTile - 1) / kTile, each = kSumThreads / 64;
+  // One launch for up to 16384 tokens (a chain drawn from them: 10.6 us, divided 11.4; 48
+  // chains: 13.0 and 14.2; 65536 tokens: 23 and 18), and from 192 sequences on (200 of
+  // 65536 tokens: 30 and 35).
+  if (a.vocab <= 16 * kTile || a.n_seqs >= 192) {
+    if (a.draft)
+      hipLaunchKernelGGL((verify_whole<T, true>), dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL((verify_whole<T, false>), dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a);
+    return hipGetLastError();
+  }
   const int shares = std::max(1, std::min((tiles + each - 1) / each, 2048 / a.n_seqs));
   const dim3 grid(static_cast<unsigned>(a.n_seqs) * shares);
   if (a.draft) {
