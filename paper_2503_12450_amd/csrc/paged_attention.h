@@ -204,31 +204,38 @@ __device__ __forceinline__ Row make_row(const AttnArgs& a, const Tile& t, int hk
   return r;
 }
 
-// The new tokens that a lane's row (row i of the tile) sees go to `nodes`, kTreeWords
-// words of LDS for it alone that its wave reads; its depth bounds what it sees of the
-// past.  The parents of the tree's nodes lie in the wave's registers, 64 to a word's
-// register, and every lane walks up from its node by lane permutes: as many steps
-// as the deepest has ancestors (at most kMaxTree: a parent comes before its child).
-// All lanes take part.
-__device__ __forceinline__ void add_nodes(const AttnArgs& a, const Tile& t, int i, uint64_t* nodes, Row& row) {
-  const int lane = threadIdx.x & 63;
-  const int node = div_by(t.r0 + min(i, t.n - 1), a.by_group.magic, a.by_group.shift);
+// Parents of the tree's nodes, node 64 w + lane in up[w]; -1: none.
+struct Parents {
   int up[kTreeWords];
+};
+__device__ __forceinline__ Parents load_parents(const AttnArgs& a, const Tile& t) {
+  Parents r;
 #pragma unroll
   for (int w = 0; w < kTreeWords; ++w) {
-    const int k = 64 * w + lane;
-    up[w] = -1;
+    const int k = 64 * w + static_cast<int>(threadIdx.x & 63);
+    r.up[w] = -1;
     if (64 * w < t.sp.n) {
       const int p = a.parent[t.sp.row0 + min(k, t.sp.n - 1)];
-      up[w] = k < t.sp.n && p >= 0 && p < k ? p : -1;
+      r.up[w] = k < t.sp.n && p >= 0 && p < k ? p : -1;
     }
   }
+  return r;
+}
+
+// The new tokens that a lane's row (row i of the tile) sees go to `nodes`, kTreeWords
+// words of LDS for it alone that its wave reads; its depth bounds what it sees of the
+// past.  Every lane walks up from its node by lane permutes: as many steps as the
+// deepest has ancestors (at most kMaxTree: a parent comes before its child).  All
+// lanes take part.
+__device__ __forceinline__ void add_nodes(const AttnArgs& a, const Tile& t, const Parents& parents, int i,
+                                          uint64_t* nodes, Row& row) {
+  const int node = div_by(t.r0 + min(i, t.n - 1), a.by_group.magic, a.by_group.shift);
   auto above = [&](int k) {  // parent of node k (of -1: -1)
     int p = -1;
 #pragma unroll
     for (int w = 0; w < kTreeWords; ++w)
       if (64 * w < t.sp.n) {
-        const int x = __builtin_amdgcn_ds_bpermute(4 * (k & 63), up[w]);
+        const int x = __builtin_amdgcn_ds_bpermute(4 * (k & 63), parents.up[w]);
         p = k >> 6 == w ? x : p;
       }
     return p;
@@ -733,7 +740,7 @@ __global__ __launch_bounds__(64 * kWaves, DH <= 64 ? 3 : 2) void attn_many(const
   };
 
   Row row = make_row(a, tile, hk, wave * 32 + c);
-  if constexpr (kTree) add_nodes(a, tile, wave * 32 + c, nodes[wave * 32 + c], row);
+  if constexpr (kTree) add_nodes(a, tile, load_parents(a, tile), wave * 32 + c, nodes[wave * 32 + c], row);
   u32x4_t qf[G::DS];
   load_q<DH>(a, row, hg, qf);
   const Reach reach = rows_reach(a, tile, wave * 32, 32);
@@ -834,8 +841,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_few(const AttnArgs a) {
     }
   };
   RowState<DH> st;
+  Parents parents;
+  if constexpr (kTree) parents = load_parents(a, tile);
   if (from + wave < to) load_block(from + wave);
-  if constexpr (kTree) add_nodes(a, tile, c, nodes[wave * 32 + c], row);  // while they are on their way
+  if constexpr (kTree) add_nodes(a, tile, parents, c, nodes[wave * 32 + c], row);  // while they are on their way
   for (int i = from + wave; i < to; i += kWaves) {
     const uint64_t alive = alive_next;
     const int key0 = blocks.at(i) * KB;
@@ -987,6 +996,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
 #pragma unroll
       for (int t = 0; t < DT; ++t) v[r][t] = vr[r * DH + 16 * t];
   };
+  Parents parents;
+  if constexpr (kTree) parents = load_parents(a, tile);
   if (from + wave < to) {
     seek(from + wave);
     load_keys();
@@ -996,7 +1007,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_f32(const AttnArgs a) {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       Row row = make_row(a, tile, hk, 16 * qt + c);
-      add_nodes(a, tile, 16 * qt + c, nodes[wave][16 * qt + c], row);
+      add_nodes(a, tile, parents, 16 * qt + c, nodes[wave][16 * qt + c], row);
       key_lo[qt] = row.lo;
     }
   for (int i = from + wave; i < to; i += kWaves) {
@@ -1287,7 +1298,7 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   // Trees, 32 rows to a tile: the join costs more than dividing a few blocks saves (6
   // trees of 20 nodes, 12 heads of 64: 600 keys 10 us, in two parts 14; 1500 keys 15, in
   // four 17.5; 16 of 6, 8 heads of 128 on 2, 1500 keys: 24, in four 20).
-  if (kTree && p.kind == FEW && blocks < (b.d_head <= 64 ? 48 : 24)) parts = 1;
+  if (kTree && p.kind == FEW && blocks <= (b.d_head <= 64 ? 48 : 24)) parts = 1;
   parts = std::max(parts, 1l);
   const size_t per_part = static_cast<size_t>(m) * heads_q * (b.d_head + 2) * sizeof(float);
   parts = std::max(1l, std::min<long>(parts, static_cast<long>(ws_bytes / per_part)));
