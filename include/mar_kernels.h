@@ -296,7 +296,8 @@ mar_status mar_k_probabilities(int32_t dtype, const void* logits, int64_t ld, co
  * sequence's nodes from the 256th on are never kept.
  *   path[q_start[s] + k] = the k-th kept node, from 0 on, -1 behind the last
  *   kept[s] = their number (0, with next -1, if the sequence has no rows)
- * Entries of path of no sequence stay as they were.  Values of p and draft that are
+ * Entries of path of no sequence stay as they were.  Outputs must not overlap inputs
+ * or each other.  Values of p and draft that are
  * no probabilities (negative, infinite, NaN) count as 0, tokens outside [0, vocab)
  * are never kept.  Products and sums in fp64, the sums in a fixed order.  Row
  * strides, alignment and vocab as in mar_k_probabilities; m < 2^30, n_seqs <=
@@ -314,7 +315,7 @@ size_t mar_k_draft_verify_workspace_bytes(int32_t m, int32_t n_seqs, int32_t voc
  * kept[s] (path [m] ascending, as mar_k_draft_verify leaves it), and kv_len_out[s]
  * = first + kept[s] (kv_len[s] of a sequence without rows).  Nodes that path names
  * out of order or outside the sequence, and tokens without a place, are not moved.
- * kv_len_out must not be kv_len.  Pages that other sequences read must not hold
+ * kv_len_out must not overlap what is read.  Pages that other sequences read must not hold
  * new tokens, as for the store. */
 mar_status mar_k_paged_keep(int32_t dtype, const mar_paged_batch* batch, int32_t m, const int32_t* path,
                             const int32_t* kept, int32_t* kv_len_out, void* stream);
@@ -335,7 +336,9 @@ mar_status mar_k_paged_keep(int32_t dtype, const mar_paged_batch* batch, int32_t
  * number of pages that there were too few of: the last rows' entries are then -1,
  * and a copy that got none is lost with its kept tokens (they are not visible).
  * Pages taken from the old sequences by this call are free from the next one on.
- * The tables and kv_len_out must not overlap.  q_start is not read.  n_new <= 65536.
+ * Outputs must not overlap inputs or each other.  Where every layer has pages of its
+ * own under one table, each layer's call gives the same table and copies its pages.
+ * q_start is not read.  n_new <= 65536.
  * workspace: device, 16-byte aligned, of at least
  * mar_k_paged_fork_workspace_bytes; calls that may overlap need one each. */
 mar_status mar_k_paged_fork(int32_t dtype, const mar_paged_batch* batch, int32_t n_new, const int32_t* source,

@@ -259,6 +259,8 @@ mar_status mar_k_draft_verify(int32_t dtype, int32_t n_seqs, const int32_t* q_st
   if (s == MAR_OK && draft && !random) s = fail(MAR_E_ARG, "draft needs random numbers");
   if (s == MAR_OK && n_seqs > 0 && (!q_start || !kept || !next)) s = fail(MAR_E_ARG, "NULL pointer");
   if (s == MAR_OK && m > 0 && (!parent || !tokens || !path)) s = fail(MAR_E_ARG, "NULL pointer");
+  if (s == MAR_OK && m > 0 && (path == parent || path == tokens)) s = fail(MAR_E_ARG, "path must not be an input");
+  if (s == MAR_OK && n_seqs > 0 && kept == next) s = fail(MAR_E_ARG, "kept must not be next");
   if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, verify_workspace(m, n_seqs, vocab));
   if (s != MAR_OK) return s;
   const VerifyArgs a{p,    draft, q_start, parent, tokens,   random, path,   kept,
@@ -298,6 +300,8 @@ mar_status mar_k_paged_fork(int32_t dtype, const mar_paged_batch* batch, int32_t
     s = fail(MAR_E_ARG, "NULL pointer");
   if (s == MAR_OK && n_new > 0 && (table_out == b.table || kv_len_out == b.kv_len))
     s = fail(MAR_E_ARG, "table_out and kv_len_out must not be the batch's");
+  if (s == MAR_OK && n_new > 0 && (kv_len_out == source || kv_len_out == keep || kv_len_out == add))
+    s = fail(MAR_E_ARG, "kv_len_out must not be an input");
   if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, paged_fork_workspace(b, n_new));
   if (s != MAR_OK) return s;
   return device_result(launch_paged_fork(dtype, b, n_new, source, keep, add, table_out, kv_len_out, missing, workspace,

@@ -141,7 +141,7 @@ def _probs_call(**kw):
 
 def _verify_call(**kw):
     a = dict(dtype=1, n=3, q_start=PTR, m=5, vocab=100, p=PTR, ld_p=100, draft=None, ld_d=100, parent=PTR, tokens=PTR,
-             random=PTR, path=PTR, kept=PTR, next=PTR, ws=PTR, ws_bytes=1 << 30)
+             random=PTR, path=2 * PTR, kept=PTR, next=2 * PTR, ws=PTR, ws_bytes=1 << 30)
     a.update(kw)
     return B.load().mar_k_draft_verify(a["dtype"], a["n"], a["q_start"], a["m"], a["vocab"], a["p"], a["ld_p"],
                                        a["draft"], a["ld_d"], a["parent"], a["tokens"], a["random"], a["path"],
@@ -207,6 +207,8 @@ def test_probabilities_refuse(status, kw):
     (ARG, dict(p=PTR + 1)), (ARG, dict(p=None)), (ARG, dict(q_start=None)), (ARG, dict(parent=None)),
     (ARG, dict(tokens=None)), (ARG, dict(path=None)), (ARG, dict(kept=None)), (ARG, dict(next=None)),
     (WS, dict(ws=PTR + 8)), (WS, dict(ws=None, ws_bytes=1 << 30)), (WS, dict(ws_bytes=4)),
+    (ARG, dict(path=2 * PTR, parent=2 * PTR)), (ARG, dict(path=2 * PTR, tokens=2 * PTR)),
+    (ARG, dict(kept=2 * PTR, next=2 * PTR)),
 ])
 def test_verification_refuses(status, kw):
     assert _verify_call(**kw) == status
@@ -225,7 +227,8 @@ def test_keeping_refuses(status, kw):
 @pytest.mark.parametrize("status,kw", [
     (ARG, dict(dtype=2)), (ARG, dict(batch=False)), (SHAPE, dict(n=-1)), (SHAPE, dict(n=65537)),
     (ARG, dict(source=None)), (ARG, dict(table=None)), (ARG, dict(kv=None)), (ARG, dict(missing=None)),
-    (ARG, dict(table=PTR)), (ARG, dict(kv=PTR)), (WS, dict(ws=PTR + 8)), (WS, dict(ws=None)), (WS, dict(ws_bytes=16)),
+    (ARG, dict(table=PTR)), (ARG, dict(kv=PTR)), (ARG, dict(source=2 * PTR)), (ARG, dict(keep=2 * PTR)),
+    (ARG, dict(add=2 * PTR)), (WS, dict(ws=PTR + 8)), (WS, dict(ws=None)), (WS, dict(ws_bytes=16)),
 ])
 def test_forking_refuses(status, kw):
     assert _fork_call(**kw) == status
@@ -239,6 +242,7 @@ def test_nothing_to_do_is_not_an_error():
     assert _tree_call(batch=_batch(**none)) == B.MAR_OK
     assert _probs_call(m=0, x=None, out=None) == B.MAR_OK
     assert _verify_call(n=0, q_start=None, kept=None, next=None) == B.MAR_OK
+    assert _probs_call(m=0, x=None, out=None, T=None) == B.MAR_OK
     assert _keep_call(batch=_batch(**none), kept=None, out=None) == B.MAR_OK
 
 

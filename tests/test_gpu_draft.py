@@ -330,6 +330,7 @@ def _draws(seed, rows, V, kind, drawn, hits=0.5, tail=0):
     ([1], 1, "chain"), ([2, 3], 2, "chain"), ([1, 0, 4, 9], 7, "chain"), ([5] * 40, 64, "chain"),
     ([30, 64, 65, 3], 100, "tree"), ([300, 130], 50, "any"), ([12, 20, 7], 1023, "tree"), ([8, 9], 1025, "wrong"),
     ([6, 1, 11], 5003, "tree"), ([9] * 3, 40000, "chain"), ([4, 3], 2 ** 20, "tree"),
+    ([3] * 200, 20000, "tree"), ([1, 2] * 40, 16385, "chain"),
 ])
 def test_verification(dtype, mode, rows, V, kind):
     p, d, parent, tokens, random = _draws(len(rows) + V, rows, V, kind, mode == "drawn", tail=2)
@@ -451,6 +452,24 @@ def test_greedy_takes_the_first_of_equals(dtype):
     assert [g.tolist() for g in got] == [[0, 2, -1, -1], [2], [-1]]
     got = _verify(x, [0, 1, 2, 3, 4], [-1] * 4, [0] * 4)
     assert got[2].tolist() == [17, 0, -1, 0]
+
+
+def test_nothing_to_verify_or_keep():
+    """No rows at all: every sequence keeps nothing and has no next token; lengths
+    stay."""
+    none = torch.empty((0,), dtype=torch.int32, device=DEV)
+    for V in (5, 40000):
+        p, ws = torch.empty((0, V), device=DEV), torch.empty(B.draft_verify_workspace_bytes(0, 3, V), dtype=torch.uint8,
+                                                             device=DEV)
+        for r, d in ((None, None), (torch.empty(0, device=DEV), None), (torch.empty(0, device=DEV), p)):
+            kept, after = (torch.full((3,), 9, dtype=torch.int32, device=DEV) for _ in range(2))
+            B.k_draft_verify(_i32([0, 0, 0, 0]), p, none, none, none.clone(), kept, after, r, d, ws)
+            assert kept.tolist() == [0, 0, 0] and after.tolist() == [-1, -1, -1]
+        B.k_probabilities(p, p.clone())
+    c = Case(3, [0, 0], [20, 40], 1, 1, 16, 16, "bf16")
+    kv = torch.zeros(2, dtype=torch.int32, device=DEV)
+    B.k_paged_keep(c.batch(), none, _i32([5, 5]), kv)
+    assert kv.tolist() == [20, 40]
 
 
 @pytest.mark.parametrize("mode", ["points", "drawn", "greedy"])
@@ -604,6 +623,42 @@ def test_forking_many_and_much():
     _check_fork(c, g.choice(edge, 50), g.choice(edge, 50), g.choice(edge, 50))
     _check_fork(c, g.integers(0, S, 50), g.choice(edge, 50), g.choice(edge, 50))
     assert _fork(c, [])[2] == 0
+
+
+def test_pages_past_32_bit_offsets():
+    """A cache of more than 2^32 bytes, the pages of the sequences at its end: read,
+    moved and copied there as in a small one."""
+    Hk, page, dh = 2, 128, 128
+    n_pages = (2 ** 32 // (Hk * page * dh * 2)) + 70
+    k = torch.empty((n_pages, Hk, page, dh), dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    c = Tree(95, [9, 33], [200, 300], 2, 2, dh, page, "bf16", "tree", spare=6)
+    n = c.k.shape[0]
+    k[n_pages - n:], v[n_pages - n:] = c.k, c.v
+    big = B.PagedBatch(B.MarPages(k, v), _i32(np.where(c.table >= 0, c.table + n_pages - n, -1)), _i32(c.q_start),
+                       _i32(c.kv))
+    assert torch.equal(c.tree(batch=big), c.tree())
+    path = [0, 3, 5, 8] + [-1] * 5 + [1, 7, 30] + [-1] * 30
+    out = [torch.zeros(2, dtype=torch.int32, device=DEV) for _ in range(2)]
+    for b, kv in zip((big, c.batch()), out):
+        B.k_paged_keep(b, _i32(path), _i32([4, 3]), kv)
+    assert torch.equal(*out)
+    # all the small pages but the sequences' own are the lowest free ones of both: of the
+    # big cache's, the ones before them are taken by a third sequence's table
+    rest = np.arange(n_pages - n, dtype=np.int32)
+    wide = np.full((3, len(rest)), -1, dtype=np.int32)
+    wide[:2, :c.table.shape[1]] = np.where(c.table >= 0, c.table + n_pages - n, -1)
+    wide[2] = rest
+    kv_len = _i32([200, 300, len(rest) * page])
+    big = B.PagedBatch(B.MarPages(k, v), _i32(wide), _i32([0, 9, 42, 42]), kv_len)
+    table, kv, missing = (torch.zeros(s, dtype=torch.int32, device=DEV) for s in ((3, len(rest)), (3,), (1,)))
+    ws = torch.empty(B.paged_fork_workspace_bytes(big, 3), dtype=torch.uint8, device=DEV)
+    B.k_paged_fork(big, _i32([0, 0, 1]), table, kv, missing, add=_i32([1, 1, 1]), workspace=ws)
+    got = _fork(c, [0, 0, 1], None, [1, 1, 1])
+    small = _cpu(table)[:, :c.table.shape[1]]
+    assert np.array_equal(np.where(small >= 0, small - (n_pages - n), -1), got[0]) and int(missing) == got[2] == 0
+    assert torch.equal(k[n_pages - n:].view(torch.int16), c.k.view(torch.int16))
+    assert torch.equal(v[n_pages - n:].view(torch.int16), c.v.view(torch.int16))
 
 
 # --------------------------------------------------------------------------
