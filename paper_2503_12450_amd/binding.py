@@ -570,11 +570,11 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
 # drafted tokens
 # --------------------------------------------------------------------------
 
-def _ints(device, i32, n: int, **tensors) -> None:
-    """Each of the tensors (None: not given) is a dense vector of n int32 on
-    `device`."""
-    for name, t in tensors.items():
-        if t is not None and not (t.dtype is i32 and t.shape == (n,) and t.device == device and t.is_contiguous()):
+def _vectors(device, i32, *named) -> None:
+    """Each (name, tensor or None, n) is a dense vector of n int32 on `device`.  (A
+    third of the time of one _dense each.)"""
+    for name, t, n in named:
+        if t is not None and (t.dtype is not i32 or t.shape != (n,) or t.device != device or not t.is_contiguous()):
             _dense(name, t, i32, (n,), device)
 
 
@@ -619,7 +619,7 @@ def k_paged_tree_attention(batch: PagedBatch, q, parent, out, window: int = 0, s
     heads_out, ldo = _rows("out", out, dtype, m, dh, dev)
     if heads_out != heads:
         _refuse("out and q differ in width")
-    _ints(dev, batch.kv_len.dtype, m, parent=parent)
+    _vectors(dev, batch.kv_len.dtype, ("parent", parent, m))
     ws_ptr, ws_bytes = _workspace(workspace, dev)
     if (m | heads | window | sinks) >> 31:
         _int32("rows, heads, window, sinks", m, heads, window, sinks)
@@ -671,9 +671,8 @@ def k_draft_verify(q_start, p, parent, tokens, path, kept, next_token, random=No
     ldd = _vocab_rows("draft", draft, dtype, shape, dev) if draft is not None else 0
     m, vocab = shape
     n_seqs, i32 = q_start.shape[0] - 1, torch.int32
-    _ints(dev, i32, n_seqs + 1, q_start=q_start)
-    _ints(dev, i32, m, parent=parent, tokens=tokens, path=path)
-    _ints(dev, i32, n_seqs, kept=kept, next_token=next_token)
+    _vectors(dev, i32, ("q_start", q_start, n_seqs + 1), ("parent", parent, m), ("tokens", tokens, m),
+             ("path", path, m), ("kept", kept, n_seqs), ("next_token", next_token, n_seqs))
     if random is not None:
         _dense("random", random, torch.float32, (m,), dev)
     ws_ptr, ws_bytes = _workspace(workspace, dev)
@@ -691,8 +690,7 @@ def k_paged_keep(batch: PagedBatch, path, kept, kv_len_out, stream=None) -> None
     lengths that remain."""
     dev, i32, n = batch.device, batch.kv_len.dtype, batch.c.n_seqs
     m = path.shape[0] if len(path.shape) == 1 else -1
-    _ints(dev, i32, m, path=path)
-    _ints(dev, i32, n, kept=kept, kv_len_out=kv_len_out)
+    _vectors(dev, i32, ("path", path, m), ("kept", kept, n), ("kv_len_out", kv_len_out, n))
     if m >> 31:
         _int32("rows", m)
     _check(load().mar_k_paged_keep(batch.code, batch.ref, m, path.data_ptr(), kept.data_ptr(), kv_len_out.data_ptr(),
@@ -716,9 +714,9 @@ def k_paged_fork(batch: PagedBatch, source, table_out, kv_len_out, missing, keep
     max_pages], kv_len_out [n], missing [1]; source, keep, add [n]; all int32."""
     dev, i32 = batch.device, batch.kv_len.dtype
     n = source.shape[0] if len(source.shape) == 1 else -1
-    _ints(dev, i32, n, source=source, kv_len_out=kv_len_out, keep=keep, add=add)
+    _vectors(dev, i32, ("source", source, n), ("kv_len_out", kv_len_out, n), ("keep", keep, n), ("add", add, n),
+             ("missing", missing, 1))
     _dense("table_out", table_out, i32, (n, batch.c.max_pages), dev)
-    _ints(dev, i32, 1, missing=missing)
     ws_ptr, ws_bytes = _workspace(workspace, dev)
     if n >> 31:
         _int32("rows", n)
