@@ -239,6 +239,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_small(const ForkArgs a
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int p = tid + k * kPlanThreads;
+    if (p >= a.b.n_pages) break;
     names[p] = writers[p] = 0;
     lowest[p] = kPlanThreads;
     used[p] = 0;
