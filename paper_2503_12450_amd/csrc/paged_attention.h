@@ -1315,8 +1315,8 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   const long even = std::min<long>((4096 + items - 1) / items, static_cast<long>(blocks) * p.kb / 1024);
   if (p.kind != MANY && even >= 4) parts = std::max(parts, even);
   // Trees, 128 rows to a tile: two workgroups for every CU, and parts of at most 2560
-  // keys, where sequences may differ in length (32 trees of 17 to 63 nodes on 530 to
-  // 7700 keys, 32 heads of 128 on 4: 101 us, undivided 218, with 1024 keys to a part
+  // keys, where sequences may differ in length (32 trees of 16 to 59 nodes on 550 to
+  // 7850 keys, 32 heads of 128 on 4: 101 us, undivided 218, with 1024 keys to a part
   // 133; 4 trees of 64 on 20000: 106, twice as many parts 122).
   if (kTree && p.kind == MANY)
     parts = std::min({std::max<long>(512 / items, (blocks + 39) / 40), static_cast<long>(blocks) / 8,
