@@ -278,7 +278,7 @@ mar_status mar_k_probabilities(int32_t dtype, const void* logits, int64_t ld, co
  * and always kept; tokens[row] is the token of every other one; row `row` of p
  * [m, vocab] (in dtype) holds the target's probabilities of the token after it.
  * From cur = 0, weights w = p[0], W = 1 the nodes are looked at in ascending order,
- * each with parent cur:
+ * each with parent cur (a token without weight is never kept):
  *   draft NULL (a token is proposed as it is): kept if random[row] W < w[token]; if
  *     not, W -= w[token] and w[token] = 0;
  *   draft given (the children of a node were drawn from row cur of draft [m,

@@ -113,7 +113,7 @@ def verify(p: np.ndarray, q_start, parent, tokens, random=None, draft: Optional[
                 r = float(random[start + i])
                 d = None if draft is None else _proper(draft[start + node])
                 chance = r * (1.0 if d is None else (d[x] if real else 0.0)) * W
-                take = bool(chance < (w[x] if real else 0.0))
+                take = real and w[x] > 0 and bool(chance < w[x])
             if take:
                 node = i
                 line.append(i)

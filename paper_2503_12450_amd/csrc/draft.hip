@@ -406,6 +406,7 @@ __device__ __forceinline__ void tile_weights(const Values& x, const Weights<T, D
     }
   }
 }
+
 // Sums of the tiles from, from + step, ... by one wave, the next tile's values on
 // their way meanwhile: take(tile, sum).
 template <typename T, bool DRAWN, typename Take>
@@ -433,7 +434,7 @@ struct End {
 };
 
 // The walk, by every wave of the workgroup; the kept nodes go to `line` (LDS) if `write`.
-// more(weights): the sum of the weights over the vocabulary.  sums: LDS, W of each rejection.
+// sum_of(weights): their sum over the vocabulary.  sums: LDS, W of each rejection.
 template <typename T, bool DRAWN, typename Sum>
 __device__ __forceinline__ End walk(const VerifyArgs& a, const TreeRows& t, const Nodes& d, int32_t* line, bool write,
                                     double* sums, Sum&& sum_of) {
@@ -446,7 +447,8 @@ __device__ __forceinline__ End walk(const VerifyArgs& a, const TreeRows& t, cons
     double wx = w.of(of_node(d.p, i), qx);
     if (!DRAWN && had_child(d, e.node, i, of_node(d.token, i))) wx = 0.0;
     const double r = of_node(d.r, i);
-    if (DRAWN ? r * static_cast<double>(qx) * W < wx : r * W < wx) {
+    // (W is above 0 as long as the random numbers are below 1)
+    if (wx > 0.0 && (DRAWN ? r * static_cast<double>(qx) * W : r * W) < wx) {
       e.node = i;
       if (write) line[e.kept] = i;
       ++e.kept;

@@ -400,10 +400,30 @@ def test_verification_of_what_is_no_probability(mode):
 
 
 @pytest.mark.parametrize("mode", ["points", "drawn"])
-def test_verification_where_the_draft_is_the_target(mode):
+@pytest.mark.parametrize("V", [400, 30000])
+def test_random_numbers_that_are_none(mode, V):
+    """Of 1, above it, negative, infinite or NaN: the definition as it stands, no token
+    without weight."""
+    g = np.random.Generator(np.random.Philox(41))
+    rows = [9, 1, 20, 6]
+    p, d, parent, tokens, random = _draws(43, rows, V, "tree", True)
+    random[g.random(len(random)) < 0.7] = np.nan
+    odd = g.random(len(random)) < 0.5
+    random[odd] = g.choice([1.0, 7.0, -1.0, -np.inf, np.inf, 1e30], int(odd.sum()))
+    q_start = np.concatenate([[0], np.cumsum(rows)])
+    td = torch.tensor(d, device=DEV) if mode == "drawn" else None
+    got = _verify(torch.tensor(p, device=DEV), q_start, parent, tokens, random, td)
+    _same(got, OD.verify(p, q_start, parent, tokens, random, d if mode == "drawn" else None))
+    for s, n in enumerate(rows):
+        line = got[0][q_start[s]:q_start[s] + got[1][s]] + q_start[s]
+        assert np.all(p[line[:-1], tokens[line[1:]]] > 0) and p[line[-1], got[2][s]] > 0
+
+
+@pytest.mark.parametrize("mode", ["points", "drawn"])
+@pytest.mark.parametrize("V", [2000, 30000])
+def test_verification_where_the_draft_is_the_target(mode, V):
     """Drafts of a one-token target, and a draft equal to it whose token is refused
     by a random number of 1: what is left is empty, and the weights stay."""
-    V = 2000
     p = np.zeros((6, V), dtype=np.float32)
     p[:, 1111] = 1.0
     p[3:, 1111], p[3:, 7] = 0.5, 0.5
