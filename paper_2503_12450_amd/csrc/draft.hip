@@ -160,13 +160,16 @@ __global__ __launch_bounds__(kBestThreads) void row_best(const T* p, long ld, in
     at = v > top ? i : at;
     top = fmaxf(top, v);
   };
-  for (int g0 = threadIdx.x; g0 < whole; g0 += AHEAD * kBestThreads) {
+  for (int base = 0; base < whole; base += AHEAD * kBestThreads) {
     u32x4_t x16[AHEAD];
+    const int g0 = base + threadIdx.x;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
-      x16[k] = load_any(x + static_cast<long>(N) * min(g0 + k * kBestThreads, whole - 1));
+      if (base + k * kBestThreads < whole)
+        x16[k] = load_any(x + static_cast<long>(N) * min(g0 + k * kBestThreads, whole - 1));
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
+      if (base + k * kBestThreads >= whole) continue;
       const int g = min(g0 + k * kBestThreads, whole - 1);  // the last one again changes nothing
       float v[N];
       unpack16(x16[k], v, static_cast<const T*>(nullptr));
