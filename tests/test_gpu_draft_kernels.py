@@ -170,3 +170,27 @@ def test_tokens_that_no_row_or_few_rows_see(dtype, heads, max_kv, kernel, bad, t
     assert len(below) > 1
     hit[[first + i for i in below], head, 9] = True
     assert not np.any(np.isfinite(got[hit])) and np.all(got[~hit] == was[~hit])
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 1100), ("bf16", 950), ("f32", 1100)])
+def test_more_tiles_than_one_launch(dtype, n):
+    """Sequences of two nodes that both hang on nothing, 4096 heads: either side of 2^22
+    workgroups.  A row's own token is its answer, or its parent's too: the mean of
+    both, as all scores are 0."""
+    H, dh = 4096, 16
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    k = torch.zeros((n, H, 16, dh), dtype=t, device=DEV)
+    v = torch.full_like(k, float("nan"))
+    g = torch.Generator(device=DEV).manual_seed(98)
+    want = torch.randn((2 * n, H, dh), generator=g, device=DEV).to(t)
+    v[:, :, 0], v[:, :, 1] = want[0::2], want[1::2]
+    q = torch.randn((2 * n, H * dh), generator=g, device=DEV).to(t)
+    out, i = torch.empty_like(q), np.arange(n)
+    batch = B.PagedBatch(B.MarPages(k, v), _i32(i[:, None]), _i32(2 * np.arange(n + 1)), _i32(np.full(n, 2)))
+    B.k_paged_tree_attention(batch, q, torch.full((2 * n,), -1, dtype=torch.int32, device=DEV), out)
+    assert torch.equal(out, want.view(2 * n, -1))
+    B.k_paged_tree_attention(batch, q, _i32(np.tile([-1, 0], n)), out)
+    assert torch.equal(out[0::2], want[0::2].reshape(n, -1))
+    mean = (want[0::2].float() + want[1::2].float()) / 2
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23   # the output's rounding (f32: two sums'); the 1% holds those of 32 bits
+    assert torch.all((out[1::2].float() - mean.view(n, -1)).abs() <= half * mean.view(n, -1).abs() * 1.01 + 1e-38)
