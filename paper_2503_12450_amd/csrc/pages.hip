@@ -248,7 +248,9 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_small(const ForkArgs a
   // rows that keep all of their sequence hold what it holds
   if (!a.keep && r.held > 0) atomicAdd(heirs + r.seq, 1);
   __syncthreads();
-  const int total = (a.b.n_seqs + (a.keep ? a.n_new : 0)) * a.width;
+  // (a batch without sequences has no table, whose first entries are read below whatever
+  // a slot is for; no new row holds a page then)
+  const int total = a.b.n_seqs > 0 ? (a.b.n_seqs + (a.keep ? a.n_new : 0)) * a.width : 0;
   for (int k0 = tid; k0 < total; k0 += 4 * kPlanThreads) {
     int page[4], count[4];  // rows that name the page; -1: the sequence itself
 #pragma unroll

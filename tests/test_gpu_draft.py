@@ -627,6 +627,30 @@ def test_forking_keeps_the_page_of_the_only_writer():
     assert got[1, 1] == t[1, 1] and got[1, 2] not in t
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,n_pages", [(1, 3), (5, 6), (5, 40), (1024, 8192), (1025, 2000), (9, 8193)])
+def test_forking_a_batch_without_sequences(dtype, n, n_pages):
+    """The first sequences of an empty pool, in the form that plans in one workgroup and in
+    the other: no table and no lengths are there to be read."""
+    page, width = 16, 3
+    k = torch.full((n_pages, 1, page, 16), 3.0, dtype=TDT[dtype], device=DEV)
+    v = torch.full_like(k, 4.0)
+    empty = torch.zeros((0, width), dtype=torch.int32, device=DEV)
+    batch = B.PagedBatch(B.MarPages(k, v), empty, _i32([0]), _i32(np.zeros(0)), max_kv=width * page)
+    g = np.random.Generator(np.random.Philox(n))
+    source, keep, add = g.integers(-1, 3, n), g.integers(-1, 70, n), g.integers(-1, 70, n)
+    for some in ((None, None), (None, add), (keep, None), (keep, add)):
+        want = OD.fork([_bits(k), _bits(v)], _cpu(empty), [], source, *some, width * page)
+        table = torch.full((n, width), -7, dtype=torch.int32, device=DEV)
+        kv, missing = (torch.full((x,), -7, dtype=torch.int32, device=DEV) for x in (n, 1))
+        ws = torch.empty(B.paged_fork_workspace_bytes(batch, n), dtype=torch.uint8, device=DEV)
+        B.k_paged_fork(batch, _i32(source), table, kv, missing, *(None if x is None else _i32(x) for x in some),
+                       workspace=ws)
+        torch.cuda.synchronize()
+        assert np.array_equal(_cpu(table), want[0]) and np.array_equal(_cpu(kv), want[1]) and int(missing) == want[2]
+    assert torch.all(k == 3.0) and torch.all(v == 4.0)
+
+
 def test_forking_many_and_much():
     """More rows than a step of the plan, more pages than one too, nonsense in the
     tables."""
