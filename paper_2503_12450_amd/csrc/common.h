@@ -112,8 +112,10 @@ __device__ __forceinline__ double wave_sum(double v) {
 
 // Workgroups of one launch at most: the runtime refuses a launch of 2^32
 // threads or more, so a grid that depends on sizes of the caller's choice is
-// cut into launches of this many workgroups (of up to 512 threads).
+// cut into launches of this many workgroups (of up to 512 threads; of more: of
+// max_grid, 2^31 threads).
 constexpr long kMaxGrid = 1l << 22;
+constexpr long max_grid(int threads) { return threads <= 512 ? kMaxGrid : (1l << 31) / threads; }
 
 // The thread-local message behind mar_last_error(): cleared at the start of
 // every C entry point, set by a failing one (never allocates).

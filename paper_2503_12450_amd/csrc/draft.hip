@@ -805,8 +805,9 @@ namespace {
 template <typename T, int THREADS, int HELD>
 hipError_t launch_rows(const void* logits, long ld, const float* temperature, int m, int vocab, float* out, long ld_out,
                        hipStream_t st) {
-  for (long first = 0; first < m; first += kMaxGrid) {
-    const dim3 part(static_cast<unsigned>(std::min(kMaxGrid, m - first)));
+  constexpr long most = max_grid(THREADS);
+  for (long first = 0; first < m; first += most) {
+    const dim3 part(static_cast<unsigned>(std::min(most, m - first)));
     hipLaunchKernelGGL((probabilities<T, THREADS, HELD>), part, dim3(THREADS), 0, st, static_cast<const T*>(logits), ld,
                        temperature, static_cast<int>(first), vocab, out, ld_out);
     const hipError_t e = hipGetLastError();

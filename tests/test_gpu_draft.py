@@ -280,6 +280,25 @@ def test_probabilities_in_place():
     assert torch.equal(x, out)
 
 
+def test_probabilities_of_more_rows_than_one_launch():
+    """2^22 and three rows of 2049 tokens, in place: the rows at the borders of launches
+    against the oracle, the rest (all zeros before) 1 / 2049 within the division's and
+    the product's rounding; the row's sum is exact."""
+    V, m = 2049, 2 ** 22 + 3
+    x = torch.zeros((m, V), device=DEV)
+    rows = [0, 2 ** 21 - 1, 2 ** 21, 2 ** 22 - 1, 2 ** 22, m - 1]
+    some = _normal(12, (len(rows), V), "f32", 3.0)
+    for k, r in enumerate(rows):
+        x[r] = some[k]
+    B.k_probabilities(x, x)
+    _check_probabilities(np.stack([_f64(x[r]) for r in rows]), _f64(some), None)
+    for r in rows:
+        x[r] = 1.0 / V
+    for part in x.split(2 ** 19):
+        low, high = torch.aminmax(part)
+        assert abs(float(low) * V - 1) <= 2.0 ** -22 and abs(float(high) * V - 1) <= 2.0 ** -22
+
+
 # --------------------------------------------------------------------------
 # Verification
 # --------------------------------------------------------------------------
