@@ -266,7 +266,8 @@ size_t mar_k_paged_tree_attention_workspace_bytes(int32_t dtype, const mar_paged
  * is not above 2^-100 (0, negative, NaN) the row's first largest value gets 1 and
  * the rest 0 (NaN is never the largest; a row without a value above -infinity
  * is zeros).  Otherwise -infinity has probability 0, and a row with a NaN or
- * +infinity, or without a finite value, is NaN.  Any row strides from vocab on
+ * +infinity, or without a finite value, is NaN.  Of T = +infinity all finite values
+ * of a row get the same.  Any row strides from vocab on
  * (< 2^31, elements); logits and out aligned to their elements; out may be logits
  * itself in fp32 (same pointer and stride), else they must not overlap.  m <
  * 2^30, 1 <= vocab <= 2^20. */

@@ -72,7 +72,7 @@ def probabilities(logits: np.ndarray, temperature=None) -> np.ndarray:
                 out[r, int(np.argmax(known))] = 1.0
             continue
         with np.errstate(invalid="ignore"):
-            e = np.exp((x[r] - np.max(x[r])) / T)
+            e = np.where(x[r] == -np.inf, 0.0, np.exp((x[r] - np.max(x[r])) / T))
             out[r] = e / e.sum()
     return out
 

@@ -11,6 +11,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLowest = -3.40282347e38f;
 constexpr float kCold = 0x1p-100f;  // temperatures up to here count as 0: 1 / T stays finite
+constexpr float kLeast = 0x1p-149f;  // 2 log2(e) / T at least, see probabilities
 
 // Rows of any length start at any element: sixteen bytes from there.
 typedef uint32_t any_f32x4_t __attribute__((ext_vector_type(4), aligned(4)));
@@ -40,6 +41,17 @@ __device__ __forceinline__ void better(float& v, int& i, float v2, int i2) {
 // pieces of a row stay in registers between the passes, so that it is read once
 // (600 rows of 65536 in bf16, 236 MB: 56 us, 4.2 TB/s; read twice 68; with streaming
 // stores 80); what a longer row has beyond them is read again.
+//
+// The exponent is (x / 2 - max / 2) (2 log2(e) / T): x - max itself passes the largest
+// fp32 number where logits lie further apart, which a temperature of 10^37 and more still
+// weighs.  (One FMA in place of the difference, and as exact.)  The factor stays
+// above 0, so that -infinity weighs 0 at an infinite temperature too; finite logits then
+// weigh the same but for 2^-21 at the most.
+//   Four roundings of the exponent (log2(e), the factor, the difference, the product)
+// make a probability 2^-a off by up to 4 a ln2 2^-24 of itself, exp2 and the division by
+// 2^-23 more: 1.3e-7 of the whole on rows of 65536 normal logits (the same formula with
+// the difference divided by T and then exp: 4.5e-8), as 1 / T once a row costs no division
+// for every logit.
 // ---------------------------------------------------------------------------
 template <typename T, int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void probabilities(const T* logits, long ld, const float* temperature, int first,
@@ -52,7 +64,7 @@ __global__ __launch_bounds__(THREADS) void probabilities(const T* logits, long l
   float* y = out + row * ld_out;
   const float temp = temperature ? temperature[row] : 1.f;
   const bool cold = !(temp > kCold);
-  const float scale = cold ? 0.f : kLog2e / temp;
+  const float scale = cold ? 0.f : fmaxf(2.f * kLog2e / temp, kLeast);
   const int wave = threadIdx.x >> 6, whole = vocab / N, tid = threadIdx.x;
   // the piece g of the row, v[0 .. n) its elements
   u32x4_t held[HELD];
@@ -116,7 +128,8 @@ __global__ __launch_bounds__(THREADS) void probabilities(const T* logits, long l
   if ((tid & 63) == 0) sm[wave] = top;
   __syncthreads();
   for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm[w]);
-  auto weight = [&](float v) { return __builtin_amdgcn_exp2f((v - top) * scale); };
+  const float half_top = .5f * top;
+  auto weight = [&](float v) { return __builtin_amdgcn_exp2f(fmaf(v, .5f, -half_top) * scale); };
   float sum = 0.f;
   each([&](const float* v, int) {
 #pragma unroll

@@ -118,6 +118,13 @@ def test_probabilities_by_hand():
     np.testing.assert_allclose(got, [[0.25, 0.75], [1, 0], [0, 1], [0, 0]])
 
 
+def test_probabilities_by_hand_at_an_infinite_temperature():
+    inf = np.inf
+    got = OD.probabilities(np.array([[0.0, 9.0, -inf], [-3e38, 3e38, -inf], [-inf, -inf, -inf], [1.0, inf, -inf]]),
+                           [inf] * 4)
+    np.testing.assert_array_equal(got, [[0.5, 0.5, 0], [0.5, 0.5, 0], [np.nan] * 3, [np.nan] * 3])
+
+
 # --------------------------------------------------------------------------
 # Refusals through the C entry points
 # --------------------------------------------------------------------------

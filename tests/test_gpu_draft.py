@@ -280,6 +280,42 @@ def test_probabilities_in_place():
     assert torch.equal(x, out)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_probabilities_at_an_infinite_temperature(dtype):
+    """Every finite logit weighs the same, whatever its value, and -infinity nothing."""
+    inf, V = float("inf"), 2100
+    big = torch.finfo(TDT[dtype]).max
+    x = _normal(8, (8, V), dtype, 4.0)
+    x[1, 1::2] = -inf
+    x[2, :V - 1] = -inf
+    x[3, ::3], x[3, 1::3], x[3, 2::3] = big, -big, -inf
+    x[4] = -inf
+    x[5, 7] = float("nan")
+    x[6, 8] = inf
+    x[7, :2050] = -big
+    out = torch.empty((8, V), device=DEV)
+    B.k_probabilities(x, out, torch.full((8,), inf, device=DEV))
+    _check_probabilities(_f64(out), _f64(x), np.full(8, inf))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_probabilities_of_logits_across_the_whole_range(dtype):
+    """Logits whose difference passes the largest fp32 number, at temperatures that it
+    does not outweigh."""
+    V, big = 2100, torch.finfo(TDT[dtype]).max
+    x = _normal(9, (6, V), dtype, 1.0)
+    x *= 0.9 * big / float(x.abs().max())
+    x[1, 5], x[1, 6] = big, -big
+    x[2, ::2], x[2, 1::2] = big, -big
+    x[3] = -big
+    x[4, 3::5] = -float("inf")
+    out = torch.empty((6, V), device=DEV)
+    for t in (1e38, 3.4e38, 2e37, 1.0):
+        temp = np.full(6, t, dtype=np.float32)
+        B.k_probabilities(x, out, torch.tensor(temp, device=DEV))
+        _check_probabilities(_f64(out), _f64(x), temp)
+
+
 def test_probabilities_of_more_rows_than_one_launch():
     """2^22 and three rows of 2049 tokens, in place: the rows at the borders of launches
     against the oracle, the rest (all zeros before) 1 / 2049 within the division's and
