@@ -308,7 +308,8 @@ mar_status mar_k_draft_verify(int32_t dtype, int32_t n_seqs, const int32_t* q_st
                               const void* p, int64_t ld_p, const void* draft, int64_t ld_draft, const int32_t* parent,
                               const int32_t* tokens, const float* random, int32_t* path, int32_t* kept, int32_t* next,
                               void* workspace, size_t workspace_bytes, void* stream);
-/* (0 also if an argument is refused; mar_last_error() then says why.) */
+/* (0 also if an argument is refused; mar_last_error() then says why.  No less for
+ * more rows, sequences or tokens: room for the largest batch does for the others.) */
 size_t mar_k_draft_verify_workspace_bytes(int32_t m, int32_t n_seqs, int32_t vocab);
 
 /* The kept nodes' keys and values moved together: with first = kv_len - n as

@@ -776,22 +776,25 @@ __global__ __launch_bounds__(64) void verify_best(const VerifyArgs a, const int3
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
+// One launch for up to 16384 tokens (a chain drawn from them: 10.6 us, divided 11.4; 48
+// chains: 13.0 and 14.2; 65536 tokens: 23 and 18), and from 192 sequences on (200 of
+// 65536 tokens: 30 and 35).  It leaves nothing in the workspace.
+constexpr int kDividedVocab = 16 * kTile, kDividedSeqs = 191;  // above, up to
+bool in_one_launch(int n_seqs, int vocab) { return vocab <= kDividedVocab || n_seqs > kDividedSeqs; }
+
 template <typename T>
 hipError_t launch_drawn(const VerifyArgs& a, hipStream_t st) {
-  Header* headers = static_cast<Header*>(a.ws);
-  double* sums = reinterpret_cast<double*>(static_cast<char*>(a.ws) + up16(sizeof(Header) * a.n_seqs));
-  // a tile to a wave, but no more workgroups than fill the chip a few times
-  const int tiles = (a.vocab + kTile - 1) / kTile, each = kSumThreads / 64;
-  // One launch for up to 16384 tokens (a chain drawn from them: 10.6 us, divided 11.4; 48
-  // chains: 13.0 and 14.2; 65536 tokens: 23 and 18), and from 192 sequences on (200 of
-  // 65536 tokens: 30 and 35).
-  if (a.vocab <= 16 * kTile || a.n_seqs >= 192) {
+  if (in_one_launch(a.n_seqs, a.vocab)) {
     if (a.draft)
       hipLaunchKernelGGL((verify_whole<T, true>), dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a);
     else
       hipLaunchKernelGGL((verify_whole<T, false>), dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a);
     return hipGetLastError();
   }
+  Header* headers = static_cast<Header*>(a.ws);
+  double* sums = reinterpret_cast<double*>(static_cast<char*>(a.ws) + up16(sizeof(Header) * a.n_seqs));
+  // a tile to a wave, but no more workgroups than fill the chip a few times
+  const int tiles = (a.vocab + kTile - 1) / kTile, each = kSumThreads / 64;
   const int shares = std::max(1, std::min((tiles + each - 1) / each, 2048 / a.n_seqs));
   const dim3 grid(static_cast<unsigned>(a.n_seqs) * shares);
   if (a.draft) {
@@ -807,10 +810,13 @@ hipError_t launch_drawn(const VerifyArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// The rows' maxima (greedy), or what the divided form's kernels leave for each other: for
+// as many of the sequences as it takes, so that room for many is room for few.
 size_t verify_workspace(int m, int n_seqs, int vocab) {
-  const size_t tiles = (static_cast<size_t>(vocab) + kTile - 1) / kTile;
-  return std::max(up16(sizeof(int32_t) * static_cast<size_t>(m)),
-                  up16(sizeof(Header) * static_cast<size_t>(n_seqs)) + sizeof(double) * n_seqs * tiles);
+  const size_t best = up16(sizeof(int32_t) * static_cast<size_t>(m));
+  if (vocab <= kDividedVocab) return best;
+  const size_t seqs = std::min(n_seqs, kDividedSeqs), tiles = (static_cast<size_t>(vocab) + kTile - 1) / kTile;
+  return std::max(best, up16(sizeof(Header) * seqs) + sizeof(double) * seqs * tiles);
 }
 
 namespace {

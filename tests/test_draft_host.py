@@ -262,6 +262,28 @@ def test_the_workspaces_are_sized():
             B.draft_verify_workspace_bytes(*bad)
 
 
+@pytest.mark.parametrize("m", [0, 1, 100, 2 ** 30 - 1])
+@pytest.mark.parametrize("n,vocab", [(1, 16384), (65536, 5), (3, 100)])
+def test_verification_of_few_tokens_asks_for_the_maxima_alone(m, n, vocab):
+    need = -(-4 * m // 16) * 16
+    assert B.draft_verify_workspace_bytes(m, n, vocab) == need
+    if m:
+        assert _verify_call(m=m, n=n, vocab=vocab, ld_p=vocab, ws_bytes=need - 1) == WS
+
+
+def test_verification_of_more_asks_for_its_sums():
+    """A header of 256 sums and a sum for every 1024 tokens, to a sequence: of up to 191
+    of them, as more are taken in one launch.  Never less for more."""
+    for n, vocab in ((191, 2 ** 20), (1, 16385), (10, 65536), (65536, 2 ** 20)):
+        some = min(n, 191)
+        least = some * (8 * 256 + 8 * -(-vocab // 1024))
+        assert least <= B.draft_verify_workspace_bytes(5, n, vocab) <= least + 16 * some + 32
+        assert B.draft_verify_workspace_bytes(2 ** 28, n, vocab) == 2 ** 30
+    sizes = [[B.draft_verify_workspace_bytes(5, n, vocab) for n in (1, 100, 191, 192, 65536)]
+             for vocab in (100, 16384, 16385, 50000, 2 ** 20)]
+    assert np.all(np.diff(sizes, axis=0) >= 0) and np.all(np.diff(sizes, axis=1) >= 0)
+
+
 # --------------------------------------------------------------------------
 # Refusals of the binding
 # --------------------------------------------------------------------------
