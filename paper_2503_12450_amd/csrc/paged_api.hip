@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdarg>
+#include <initializer_list>
 
 #include "../../include/mar_kernels.h"
 #include "draft.h"
@@ -121,6 +122,49 @@ mar_status check_workspace(const void* ws, size_t have, size_t need) {
   return MAR_OK;
 }
 
+// Bytes that a call reads or writes throughout (NULL or 0: none).
+struct Range {
+  const char* name;
+  const void* at;
+  size_t bytes;
+};
+Range vector_of(const char* name, const void* p, int64_t n) {
+  return {name, p, p ? static_cast<size_t>(n) * sizeof(int32_t) : 0};
+}
+// m rows of n elements of es bytes; none if gaps lie between the rows, where others may be.
+Range rows_of(const char* name, const void* p, int64_t ld, int32_t m, int64_t n, unsigned es) {
+  return {name, p, p && (ld == n || m <= 1) ? static_cast<size_t>(m) * n * es : 0};
+}
+Range pages_of(const char* name, const void* p, const PagedBatch& b, int32_t dtype) {
+  return {name, p, (static_cast<size_t>(b.n_pages) * b.n_heads * b.d_head << b.page_shift) * (dtype == MAR_BF16 ? 2 : 4)};
+}
+bool meet(const Range& a, const Range& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return a.bytes && b.bytes && (x <= y ? y - x < a.bytes : x - y < b.bytes);
+}
+// Outputs (the first `outs`) that overlap one another or what is read are refused: a
+// workgroup would read what another one has written already.
+mar_status check_apart(std::initializer_list<Range> all, size_t outs) {
+  for (const Range* a = all.begin(); a != all.begin() + outs; ++a)
+    for (const Range* b = a + 1; b != all.end(); ++b)
+      if (meet(*a, *b)) return fail(MAR_E_ARG, "%s must not overlap %s", a->name, b->name);
+  return MAR_OK;
+}
+// The same for out and in, m rows of n elements each: exact for dense rows and where the
+// rows lie equally far apart (columns of one matrix are apart).
+mar_status check_rows_apart(const char* out_name, const void* out, int64_t ld_out, unsigned es_out, const char* in_name,
+                            const void* in, int64_t ld_in, unsigned es_in, int32_t m, int64_t n) {
+  bool overlap = meet(rows_of("", out, ld_out, m, n, es_out), rows_of("", in, ld_in, m, n, es_in));
+  const int64_t ld = ld_out * es_out;
+  if (m > 0 && ld == ld_in * es_in) {
+    const int64_t far = reinterpret_cast<intptr_t>(in) - reinterpret_cast<intptr_t>(out);
+    const int64_t rows = far >= 0 ? far / ld : -((ld - 1 - far) / ld), columns = far - rows * ld;  // columns >= 0
+    overlap |= columns < n * es_out && rows > -m && rows < m;
+    overlap |= columns + n * es_in > ld && rows + 1 > -m && rows + 1 < m;
+  }
+  return overlap ? fail(MAR_E_ARG, "%s must not overlap %s", out_name, in_name) : MAR_OK;
+}
+
 mar_status take_fork(const mar_paged_batch* batch, int32_t n_new, PagedBatch* b) {
   const mar_status s = take_batch(batch, b);
   if (s != MAR_OK) return s;
@@ -219,6 +263,11 @@ mar_status mar_k_paged_tree_attention(int32_t dtype, const mar_paged_batch* batc
   if (s == MAR_OK && m > 0 && out == q) s = fail(MAR_E_ARG, "out must not be q");
   if (s == MAR_OK && !workspace && workspace_bytes) s = fail(MAR_E_WORKSPACE, "workspace is NULL");
   if (s == MAR_OK && !aligned16(workspace)) s = fail(MAR_E_WORKSPACE, "workspace must be 16-byte aligned");
+  const unsigned es = dtype == MAR_BF16 ? 2 : 4;
+  const int64_t width = static_cast<int64_t>(n_heads_q) * b.d_head;
+  if (s == MAR_OK && b.n_seqs > 0) s = check_rows_apart("out", out, ld_out, es, "q", q, ld_q, es, m, width);
+  if (s == MAR_OK && b.n_seqs > 0)
+    s = check_apart({rows_of("out", out, ld_out, m, width, es), vector_of("parent", parent, m)}, 1);
   if (s != MAR_OK) return s;
   return device_result(launch_tree_attention(dtype, b, m, n_heads_q, q, ld_q, parent, window, sinks, workspace,
                                              workspace_bytes, out, ld_out, static_cast<hipStream_t>(stream)),
@@ -234,6 +283,10 @@ mar_status mar_k_probabilities(int32_t dtype, const void* logits, int64_t ld, co
   if (s == MAR_OK) s = check_vocab_rows("out", out, ld_out, m, vocab, 4);
   if (s == MAR_OK && m > 0 && static_cast<const void*>(out) == logits && (dtype != MAR_F32 || ld != ld_out))
     s = fail(MAR_E_ARG, "out may be logits only in fp32 with the same row stride");
+  if (s == MAR_OK && static_cast<const void*>(out) != logits)
+    s = check_rows_apart("out", out, ld_out, 4, "logits", logits, ld, dtype == MAR_BF16 ? 2 : 4, m, vocab);
+  if (s == MAR_OK)
+    s = check_apart({rows_of("out", out, ld_out, m, vocab, 4), vector_of("temperature", temperature, m)}, 1);
   if (s != MAR_OK) return s;
   return device_result(launch_probabilities(dtype, logits, ld, temperature, m, vocab, out, ld_out,
                                             static_cast<hipStream_t>(stream)),
@@ -259,9 +312,14 @@ mar_status mar_k_draft_verify(int32_t dtype, int32_t n_seqs, const int32_t* q_st
   if (s == MAR_OK && draft && !random) s = fail(MAR_E_ARG, "draft needs random numbers");
   if (s == MAR_OK && n_seqs > 0 && (!q_start || !kept || !next)) s = fail(MAR_E_ARG, "NULL pointer");
   if (s == MAR_OK && m > 0 && (!parent || !tokens || !path)) s = fail(MAR_E_ARG, "NULL pointer");
-  if (s == MAR_OK && m > 0 && (path == parent || path == tokens)) s = fail(MAR_E_ARG, "path must not be an input");
-  if (s == MAR_OK && n_seqs > 0 && kept == next) s = fail(MAR_E_ARG, "kept must not be next");
-  if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, verify_workspace(m, n_seqs, vocab));
+  const size_t need = s == MAR_OK ? verify_workspace(m, n_seqs, vocab) : 0;
+  if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, need);
+  if (s == MAR_OK && n_seqs > 0)
+    s = check_apart({vector_of("path", path, m), vector_of("kept", kept, n_seqs), vector_of("next", next, n_seqs),
+                     {"workspace", workspace, need}, vector_of("q_start", q_start, n_seqs + 1),
+                     vector_of("parent", parent, m), vector_of("tokens", tokens, m), vector_of("random", random, m),
+                     rows_of("p", p, ld_p, m, vocab, es), rows_of("draft", draft, ld_draft, m, vocab, es)},
+                    4);
   if (s != MAR_OK) return s;
   const VerifyArgs a{p,    draft, q_start, parent, tokens,   random, path,   kept,
                      next, workspace, ld_p, ld_draft, m, n_seqs, vocab};
@@ -276,7 +334,13 @@ mar_status mar_k_paged_keep(int32_t dtype, const mar_paged_batch* batch, int32_t
   if (s == MAR_OK) s = take_batch(batch, &b);
   if (s == MAR_OK && (m < 0 || m >= kMaxTokens)) s = fail(MAR_E_SHAPE, "need 0 <= m < 2^30");
   if (s == MAR_OK && ((m > 0 && !path) || (b.n_seqs > 0 && (!kept || !kv_len_out)))) s = fail(MAR_E_ARG, "NULL pointer");
-  if (s == MAR_OK && b.n_seqs > 0 && kv_len_out == b.kv_len) s = fail(MAR_E_ARG, "kv_len_out must not be kv_len");
+  const int64_t n = s == MAR_OK ? b.n_seqs : 0;
+  if (n > 0)
+    s = check_apart({vector_of("kv_len_out", kv_len_out, n), vector_of("kv_len", b.kv_len, n),
+                     vector_of("q_start", b.q_start, n + 1), vector_of("table", b.table, n * b.max_pages),
+                     vector_of("path", path, m), vector_of("kept", kept, n), pages_of("k", b.k, b, dtype),
+                     pages_of("v", b.v, b, dtype)},
+                    1);
   if (s != MAR_OK) return s;
   return device_result(launch_paged_keep(dtype, b, m, path, kept, kv_len_out, static_cast<hipStream_t>(stream)),
                        "paged keep");
@@ -298,11 +362,16 @@ mar_status mar_k_paged_fork(int32_t dtype, const mar_paged_batch* batch, int32_t
   if (s == MAR_OK) s = take_fork(batch, n_new, &b);
   if (s == MAR_OK && (!missing || (n_new > 0 && (!source || !table_out || !kv_len_out))))
     s = fail(MAR_E_ARG, "NULL pointer");
-  if (s == MAR_OK && n_new > 0 && (table_out == b.table || kv_len_out == b.kv_len))
-    s = fail(MAR_E_ARG, "table_out and kv_len_out must not be the batch's");
-  if (s == MAR_OK && n_new > 0 && (kv_len_out == source || kv_len_out == keep || kv_len_out == add))
-    s = fail(MAR_E_ARG, "kv_len_out must not be an input");
-  if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, paged_fork_workspace(b, n_new));
+  const size_t need = s == MAR_OK ? paged_fork_workspace(b, n_new) : 0;
+  if (s == MAR_OK) s = check_workspace(workspace, workspace_bytes, need);
+  if (s == MAR_OK)
+    s = check_apart({vector_of("table_out", table_out, static_cast<int64_t>(n_new) * b.max_pages),
+                     vector_of("kv_len_out", kv_len_out, n_new), vector_of("missing", missing, 1),
+                     {"workspace", workspace, need}, pages_of("k", b.k, b, dtype), pages_of("v", b.v, b, dtype),
+                     vector_of("table", b.table, static_cast<int64_t>(b.n_seqs) * b.max_pages),
+                     vector_of("kv_len", b.kv_len, b.n_seqs), vector_of("source", source, n_new),
+                     vector_of("keep", keep, n_new), vector_of("add", add, n_new)},
+                    4);
   if (s != MAR_OK) return s;
   return device_result(launch_paged_fork(dtype, b, n_new, source, keep, add, table_out, kv_len_out, missing, workspace,
                                          static_cast<hipStream_t>(stream)),

@@ -242,6 +242,98 @@ def test_forking_refuses(status, kw):
     assert B.load().mar_last_error()
 
 
+def _refused_overlap(status, *names):
+    said = B.load().mar_last_error().decode()
+    assert status == ARG and all(n in said for n in names) and "overlap" in said, (status, said)
+
+
+def _apart(**sizes):
+    """Addresses of ranges of these sizes, 64 bytes between them."""
+    at, out = 1 << 20, {}
+    for name, n in sizes.items():
+        out[name] = at
+        at += -(-n // 64) * 64 + 64
+    return out
+
+
+V = dict(n=3, m=5, vocab=20, ld_p=20, ld_d=20, dtype=0)
+V_ARGS = dict(path=20, kept=12, next=12, ws=4096, q_start=16, parent=20, tokens=20, random=20, p=400, draft=400)
+
+
+@pytest.mark.parametrize("out", ["path", "kept", "next", "ws"])
+@pytest.mark.parametrize("other", list(V_ARGS))
+def test_verification_refuses_outputs_that_overlap(out, other):
+    """The last word of one in the first of the other, and the reverse; of a workspace,
+    what the call needs of it."""
+    if out == other:
+        return
+    at = _apart(**V_ARGS)
+    need = B.draft_verify_workspace_bytes(V["m"], V["n"], V["vocab"])
+    size = dict(V_ARGS, ws=need)
+    if out == "ws":  # aligned, it stays
+        moved = [{other: at["ws"] + need - 4}]
+    else:
+        moved = [{out: at[other] - size[out] + 4}, {out: at[other] + size[other] - 4}]
+    for places in moved:
+        status = _verify_call(**V, **dict(at, **places), ws_bytes=4096)
+        _refused_overlap(status, *("workspace" if x == "ws" else x for x in (out, other)))
+
+
+def test_verification_may_leave_outputs_between_rows():
+    """What lies between the rows of p is not p's: the call goes on to the next refusal
+    (the overlap of kept and next)."""
+    at = _apart(**dict(V_ARGS, p=4000))
+    status = _verify_call(**dict(V, ld_p=200), **dict(at, path=at["p"] + 80, next=at["kept"]), ws_bytes=4096)
+    _refused_overlap(status, "kept", "next")
+
+
+@pytest.mark.parametrize("other,size", [("kv_len", 12), ("q_start", 16), ("table", 48), ("path", 20), ("kept", 12),
+                                        ("k", 10 * 2 * 16 * 64 * 2), ("v", 10 * 2 * 16 * 64 * 2)])
+def test_keeping_refuses_lengths_that_overlap(other, size):
+    sizes = dict(kv_len=12, q_start=16, table=48, path=20, kept=12, k=40960, v=40960, out=12)
+    at = _apart(**sizes)
+    for where in (at[other] - 8, at[other] + size - 4):
+        batch = _batch(**{n: at[n] for n in ("k", "v", "table", "q_start", "kv_len")})
+        _refused_overlap(_keep_call(batch=batch, path=at["path"], kept=at["kept"], out=where), "kv_len_out", other)
+
+
+@pytest.mark.parametrize("out,name", [("table_out", "table"), ("kv_len_out", "kv"), ("missing", "missing")])
+@pytest.mark.parametrize("other", ["table", "kv_len", "source", "keep", "add", "k", "v", "ws"])
+def test_forking_refuses_outputs_that_overlap(out, name, other):
+    sizes = dict(table_out=80, kv_len_out=20, missing=4, table=48, kv_len=12, source=20, keep=20, add=20, k=40960,
+                 v=40960, ws=4096)
+    at = _apart(**sizes)
+    batch = _batch(**{n: at[n] for n in ("k", "v", "table", "kv_len")})
+    need = B.load().mar_k_paged_fork_workspace_bytes(ctypes.byref(batch), 5)
+    last = dict(sizes, ws=need)[other]
+    for where in (at[other], at[other] + last - 4):
+        where = {"table_out": at["table_out"], "kv_len_out": at["kv_len_out"], "missing": at["missing"], out: where}
+        status = _fork_call(batch=batch, table=where["table_out"], kv=where["kv_len_out"], missing=where["missing"],
+                            source=at["source"], keep=at["keep"], add=at["add"], ws=at["ws"], ws_bytes=4096)
+        _refused_overlap(status, out, "workspace" if other == "ws" else other)
+
+
+def test_rows_that_overlap_are_refused():
+    """Probabilities and outputs of attention over their inputs: dense ones anywhere,
+    strided ones where columns meet."""
+    x = 1 << 20
+    for off in (-5 * 400 + 4, -400, 4, 5 * 400 - 4):                     # dense, fp32
+        _refused_overlap(_probs_call(dtype=0, x=x, out=x + off), "out", "logits")
+    _refused_overlap(_probs_call(dtype=1, x=x, out=x + 996), "out", "logits")
+    for off in (-396, 396, 800 + 396, -800 - 396, 3200 + 396, 800):      # rows 800 bytes apart, 400 wide
+        _refused_overlap(_probs_call(dtype=0, x=x, out=x + off, ld=200, ld_o=200), "out", "logits")
+    _refused_overlap(_probs_call(x=x, out=x + 4096, T=x + 4096 + 5 * 400 - 4), "out", "temperature")
+    for off in (4 * 512 + 496, -16, 512, 16):
+        _refused_overlap(_tree_call(q=x, out=x + off, ld_q=256, ld_o=256), "out", "q")
+    for off in (1008, 2 * 1024 + 496, -496):                             # rows 1024 bytes apart, 512 wide
+        _refused_overlap(_tree_call(q=x, out=x + off, ld_q=512, ld_o=512), "out", "q")
+    _refused_overlap(_tree_call(q=x, out=2 * x, parent=2 * x + 512 * 5 - 4), "out", "parent")
+    # columns of one matrix are apart, also first and last rows: the next refusal speaks
+    for off in (400, -400, 3200 + 400, -4000 - 400, 4000):
+        status = _probs_call(dtype=0, x=x, out=x + off, ld=200, ld_o=200, T=x + off, m=1)
+        _refused_overlap(status, "out", "temperature")
+
+
 def test_nothing_to_do_is_not_an_error():
     """No rows, or no sequences: nothing is enqueued and no pointer is followed."""
     none = dict(n_seqs=0, table=None, kv_len=None)
