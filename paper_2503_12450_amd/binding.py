@@ -570,11 +570,20 @@ def k_paged_attention(batch: PagedBatch, q, out, causal: bool = True, window: in
 # drafted tokens
 # --------------------------------------------------------------------------
 
+def _missing(**named) -> None:
+    """Refuses the first of the tensors that is None, if one is."""
+    for name, t in named.items():
+        if t is None:
+            _refuse(f"{name} is missing")
+
+
 def _vectors(device, i32, *named) -> None:
-    """Each (name, tensor or None, n) is a dense vector of n int32 on `device`.  (A
-    third of the time of one _dense each.)"""
+    """Each (name, tensor, n) is a dense vector of n int32 on `device`.  (A third of the
+    time of one _dense each.)"""
     for name, t, n in named:
-        if t is not None and (t.dtype is not i32 or t.shape != (n,) or t.device != device or not t.is_contiguous()):
+        if t is None:
+            _missing(**{name: t})
+        if t.dtype is not i32 or t.shape != (n,) or t.device != device or not t.is_contiguous():
             _dense(name, t, i32, (n,), device)
 
 
@@ -614,6 +623,8 @@ def k_paged_tree_attention(batch: PagedBatch, q, parent, out, window: int = 0, s
     """Attention of the rows q [m, heads * d_head], the nodes of their sequences'
     trees (parent [m] int32: number of a row's parent in its sequence, or -1), over
     the past, themselves and their ancestors."""
+    if q is None or out is None:
+        _missing(q=q, out=out)
     m, dev, dh, dtype = q.shape[0], batch.device, batch.d_head, batch.dtype
     heads, ldq = _rows("q", q, dtype, m, dh, dev)
     heads_out, ldo = _rows("out", out, dtype, m, dh, dev)
@@ -632,6 +643,8 @@ def k_probabilities(logits, out, temperature=None, stream=None) -> None:
     """out [m, vocab] fp32 = probabilities of the logits' rows at temperature [m]
     fp32 (None: 1; 0: one at the first largest logit)."""
     torch = _torch()
+    if logits is None or out is None:
+        _missing(logits=logits, out=out)
     dev, dtype, shape = logits.device, logits.dtype, logits.shape
     if len(shape) != 2:
         _refuse(f"logits: need [m, vocab], got {tuple(shape)}")
@@ -664,6 +677,8 @@ def k_draft_verify(q_start, p, parent, tokens, path, kept, next_token, random=No
     (None: greedy); draft [m, vocab]: probabilities that a node's children were
     drawn from (None: they are proposed as they are)."""
     torch = _torch()
+    if p is None or q_start is None:
+        _missing(p=p, q_start=q_start)
     dev, dtype, shape = p.device, p.dtype, p.shape
     if len(shape) != 2 or len(q_start.shape) != 1 or q_start.shape[0] < 1:
         _refuse("need p [m, vocab] and q_start [n_seqs + 1]")
@@ -689,6 +704,8 @@ def k_paged_keep(batch: PagedBatch, path, kept, kv_len_out, stream=None) -> None
     leaves them) moved together in the batch's pages; kv_len_out [seqs]: the
     lengths that remain."""
     dev, i32, n = batch.device, batch.kv_len.dtype, batch.c.n_seqs
+    if path is None:
+        _missing(path=path)
     m = path.shape[0] if len(path.shape) == 1 else -1
     _vectors(dev, i32, ("path", path, m), ("kept", kept, n), ("kv_len_out", kv_len_out, n))
     if m >> 31:
@@ -713,9 +730,14 @@ def k_paged_fork(batch: PagedBatch, source, table_out, kv_len_out, missing, keep
     tokens (None: all) and room for add[i] more (None: none).  table_out [n,
     max_pages], kv_len_out [n], missing [1]; source, keep, add [n]; all int32."""
     dev, i32 = batch.device, batch.kv_len.dtype
+    if source is None or table_out is None:
+        _missing(source=source, table_out=table_out)
     n = source.shape[0] if len(source.shape) == 1 else -1
-    _vectors(dev, i32, ("source", source, n), ("kv_len_out", kv_len_out, n), ("keep", keep, n), ("add", add, n),
-             ("missing", missing, 1))
+    _vectors(dev, i32, ("source", source, n), ("kv_len_out", kv_len_out, n), ("missing", missing, 1))
+    if keep is not None:
+        _vectors(dev, i32, ("keep", keep, n))
+    if add is not None:
+        _vectors(dev, i32, ("add", add, n))
     _dense("table_out", table_out, i32, (n, batch.c.max_pages), dev)
     ws_ptr, ws_bytes = _workspace(workspace, dev)
     if n >> 31:

@@ -442,3 +442,27 @@ def test_binding_refuses_what_the_library_cannot_see():
                  lambda: B.k_probabilities(wide, wide)]:
         with pytest.raises(B.MarError, match="32 bits"):
             call()
+
+
+def test_binding_refuses_tensors_that_are_missing():
+    pages = B.MarPages(torch.zeros(4, 2, 16, 32), torch.zeros(4, 2, 16, 32))
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)
+    table = torch.zeros((2, 2), dtype=torch.int32)
+    batch = B.PagedBatch(pages, table, i32(0, 1, 2), i32(3, 4))
+    x, p, two = torch.zeros(2, 64), torch.zeros(2, 50), i32(0, 0)
+    calls = [
+        (B.k_paged_tree_attention, dict(batch=batch, q=x, parent=two, out=x.clone()), ("q", "parent", "out")),
+        (B.k_probabilities, dict(logits=p, out=p.clone()), ("logits", "out")),
+        (B.k_draft_verify, dict(q_start=i32(0, 1, 2), p=p, parent=two, tokens=two, path=two.clone(), kept=two.clone(),
+                                next_token=two.clone()),
+         ("q_start", "p", "parent", "tokens", "path", "kept", "next_token")),
+        (B.k_paged_keep, dict(batch=batch, path=two, kept=two, kv_len_out=two.clone()), ("path", "kept", "kv_len_out")),
+        (B.k_paged_fork, dict(batch=batch, source=two, table_out=table.clone(), kv_len_out=two.clone(), missing=i32(0)),
+         ("source", "table_out", "kv_len_out", "missing")),
+    ]
+    for call, args, needed in calls:
+        for name in needed:
+            with pytest.raises(B.MarError, match=f"{name} is missing"):
+                call(**dict(args, **{name: None}))
+        with pytest.raises(B.MarError, match="current GPU"):   # all there: the next refusal
+            call(**args)
