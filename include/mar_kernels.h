@@ -248,8 +248,12 @@ size_t mar_k_paged_attention_workspace_bytes(int32_t dtype, const mar_paged_batc
  * number of a node's ancestors, the node lies at position first + depth and sees
  *   token j < first  if window == 0, or j > first + depth - window, or j < sinks,
  *   itself, and an ancestor whose position passes the same test.
- * A sequence's nodes from the 256th on are left as they were in out.  Workspace,
- * strides, roundings, empty rows and values that are not finite as there. */
+ * A sequence's nodes of numbers 256 and above are left as they were in out.
+ * Workspace, strides, roundings, empty rows and values that are not finite as there;
+ * a loose max_kv costs more here (32 trees of 37 nodes on 550 to 7850 keys, 32 heads
+ * of 128 on 4: 184 us, with 16384 for 7850 210, with 131072 259; 6 trees of 20 on 600
+ * keys, 12 heads of 64: 10 us, with 2048 14, with 131072 32).  out must not overlap
+ * q or parent. */
 mar_status mar_k_paged_tree_attention(int32_t dtype, const mar_paged_batch* batch, int32_t m, int32_t n_heads_q,
                                       const void* q, int64_t ld_q, const int32_t* parent, int32_t window,
                                       int32_t sinks, void* workspace, size_t workspace_bytes, void* out,
@@ -294,7 +298,7 @@ mar_status mar_k_probabilities(int32_t dtype, const void* logits, int64_t ld, co
  * p one after the other.  random NULL (draft too): greedy, a node is kept if
  * its token is the first largest of p[cur], which is also next (p may be
  * logits; NaN is never the largest; -1 if nothing is above -infinity).  A
- * sequence's nodes from the 256th on are never kept.
+ * sequence's nodes of numbers 256 and above are never kept.
  *   path[q_start[s] + k] = the k-th kept node, from 0 on, -1 behind the last
  *   kept[s] = their number (0, with next -1, if the sequence has no rows)
  * Entries of path of no sequence stay as they were.  Outputs must not overlap inputs
@@ -315,8 +319,9 @@ size_t mar_k_draft_verify_workspace_bytes(int32_t m, int32_t n_seqs, int32_t voc
 /* The kept nodes' keys and values moved together: with first = kv_len - n as
  * above, token first + path[k] goes to the place of token first + k for every k <
  * kept[s] (path [m] ascending, as mar_k_draft_verify leaves it), and kv_len_out[s]
- * = first + kept[s] (kv_len[s] of a sequence without rows).  Nodes that path names
- * out of order or outside the sequence, and tokens without a place, are not moved.
+ * = first + kept[s] (kv_len[s] of a sequence without rows).  Nothing is moved to the
+ * place of token first + k where path[k] <= k or names no row of the sequence, or
+ * where one of the two tokens has no place.
  * kv_len_out must not overlap what is read.  Pages that other sequences read must not hold
  * new tokens, as for the store. */
 mar_status mar_k_paged_keep(int32_t dtype, const mar_paged_batch* batch, int32_t m, const int32_t* path,

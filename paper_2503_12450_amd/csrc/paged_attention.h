@@ -471,6 +471,10 @@ __device__ __forceinline__ void softmax_step(RowState<G::DH>& st, f32x16_t (&sc)
   // where references of blocks, waves or parts meet it counts, as little as 2^-13
   // up to |m| = 2^12.  Rows past that (`rough`) take it off in every block; they
   // move by their maximum, not by p that lack it.
+  // The weights p are rounded to bf16, as the matrix units take both operands of the
+  // second product in one type; two bf16 for each would double that product.  Rows of
+  // 4000 normal keys: 1.6e-3 of the output, as much as the output's own rounding to
+  // bf16 adds (1.7e-3; 2.3e-3 together).
   u32x4_t pf[NSB][2];
   float psum;
   auto weights = [&](auto arg) {
@@ -1286,7 +1290,11 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   // through a block (one tree of 128 nodes on 8000 keys, 16 heads of 64: 25 us, tiles
   // of 128: 40; 32 of 2 nodes on 500 to 8000, 32 heads of 128 on 4: 44 and 66; of 4: 69
   // and 66; one of 20 on 131000, 16 heads on 2: 112 and 91; 32 of 40 on 8000: 456 and
-  // 285).
+  // 285).  What a window leaves of the keys does not count here: on long contexts it
+  // is read by tiles of 128, which few rows pay for (32 heads of 128 on 4, max_kv
+  // 100000: one tree of 8 in a window of 1024 takes 25 us, at max_kv 1224, so with
+  // tiles of 32, 15; 8 trees of 8 26 and 21, in a window of 4096 31 and 37; one of 128
+  // 33 and 35).
   if (kTree && p.kind != F32) p.kind = few * b.max_kv * b.d_head <= 1l << 26 ? FEW : MANY;
   // fp32: 32 rows to a tile read the keys half as often, where that still makes
   // tiles enough (500 rows in each of 4 sequences, 3500 keys, 16 heads of 64: 365
@@ -1314,10 +1322,11 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   long parts = std::min<long>((fill + items - 1) / items, blocks / (p.kind == MANY ? 4 : 8));
   const long even = std::min<long>((4096 + items - 1) / items, static_cast<long>(blocks) * p.kb / 1024);
   if (p.kind != MANY && even >= 4) parts = std::max(parts, even);
-  // Trees, 128 rows to a tile: two workgroups for every CU, and parts of at most 2560
-  // keys, where sequences may differ in length (32 trees of 16 to 59 nodes on 550 to
-  // 7850 keys, 32 heads of 128 on 4: 101 us, undivided 218, with 1024 keys to a part
-  // 133; 4 trees of 64 on 20000: 106, twice as many parts 122).
+  // Trees, 128 rows to a tile: two workgroups for every CU, and parts of about 2560
+  // keys of max_kv, where sequences may differ in length, while tiles times parts are
+  // 4096 workgroups or fewer (32 trees of 16 to 59 nodes on 550 to 7850 keys, 32 heads
+  // of 128 on 4: 101 us, undivided 218, with 1024 keys to a part 133; 4 trees of 64 on
+  // 20000: 106, twice as many parts 122).
   if (kTree && p.kind == MANY)
     parts = std::min({std::max<long>(512 / items, (blocks + 39) / 40), static_cast<long>(blocks) / 8,
                       std::max(4096 / items, 1l)});
