@@ -49,9 +49,9 @@ __device__ __forceinline__ void better(float& v, int& i, float v2, int i2) {
 // weigh the same but for 2^-21 at the most.
 //   Four roundings of the exponent (log2(e), the factor, the difference, the product)
 // make a probability 2^-a off by up to 4 a ln2 2^-24 of itself, exp2 and the division by
-// 2^-23 more: 1.3e-7 of the whole on rows of 65536 normal logits (the same formula with
-// the difference divided by T and then exp: 4.5e-8), as 1 / T once a row costs no division
-// for every logit.
+// 2^-23 more: 0.7e-7 to 1.3e-7 of the whole on rows of 32000 and 65536 logits (every
+// difference divided by T and then exp: half of that or less), as 1 / T once a row costs
+// no division for every logit.
 // ---------------------------------------------------------------------------
 template <typename T, int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void probabilities(const T* logits, long ld, const float* temperature, int first,
