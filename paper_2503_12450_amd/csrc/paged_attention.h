@@ -1293,8 +1293,7 @@ Plan make_plan(int dtype, const PagedBatch& b, int m, int heads_q, int causal, i
   // 285).  What a window leaves of the keys does not count here: on long contexts it
   // is read by tiles of 128, which few rows pay for (32 heads of 128 on 4, max_kv
   // 100000: one tree of 8 in a window of 1024 takes 25 us, at max_kv 1224, so with
-  // tiles of 32, 15; 8 trees of 8 26 and 21, in a window of 4096 31 and 37; one of 128
-  // 33 and 35).
+  // tiles of 32, 15; 8 trees of 8 26 and 21, in a window of 4096 31 and 37).
   if (kTree && p.kind != F32) p.kind = few * b.max_kv * b.d_head <= 1l << 26 ? FEW : MANY;
   // fp32: 32 rows to a tile read the keys half as often, where that still makes
   // tiles enough (500 rows in each of 4 sequences, 3500 keys, 16 heads of 64: 365
